@@ -451,6 +451,163 @@ qmoe_status qmoe_bf16_layer_forward(const uint16_t *const *wi_dense /*device [n_
                                     int n_tokens, float *y /*device*/, void *workspace /*device*/,
                                     size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------- */
+/* Around the layer: residual stream and norm, the router's choice            */
+/* ------------------------------------------------------------------------- */
+
+/* Element types of the arrays below that may be either. */
+#define QMOE_F32 0
+#define QMOE_BF16 1
+
+/*
+ * A norm over the d values of a row, its statistics in fp32:
+ *   QMOE_NORM_RMS    v / sqrt(mean(v^2) + eps) * weight + bias
+ *   QMOE_NORM_LAYER  (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight + bias
+ */
+#define QMOE_NORM_RMS 0
+#define QMOE_NORM_LAYER 1
+typedef struct qmoe_norm {
+    int32_t kind;        /* QMOE_NORM_* */
+    float eps;           /* >= 0 */
+    const float *weight; /* device fp32 [d], or NULL (= 1) */
+    const float *bias;   /* device fp32 [d], or NULL (= 0) */
+} qmoe_norm;
+
+/*
+ * The step between two calls of a block: the output of one goes into the residual stream, and the
+ * stream is normalised for the next.  For every token t < n_tokens, in fp32:
+ *   b     = sum over j < k of gate[t * k + j] * y[t * k + j]     (gate NULL: 1)
+ *   b'    = post(b)                                              (post NULL: b)
+ *   h'    = h[t] + alpha * channel_scale * b'                    (channel_scale [d], NULL: 1)
+ *   h_out[t] = h'                                                rounded once, to h_type
+ *   x[t * copies + j] = bf16(pre(h'))   for j < copies           (pre NULL: bf16(h'); of h' before its rounding)
+ * y holds the k rows of a token one after the other, as a layer call over n_tokens * k rows leaves them
+ * (y NULL: h' = h; k, gate, post, alpha and channel_scale are not looked at); x with copies = k is what such a
+ * call takes.  h_out NULL: not written; x NULL: not written, pre and copies not looked at; one of the two is needed.
+ * ld_*: elements from a row to the next, at least d.  h_out may be h itself (with the same
+ * ld); apart from that outputs overlap nothing.  Rows behind the last token are left as they were.
+ * Any d and any alignment that fits the element type; 16-byte aligned rows of whole 16 bytes are fastest.
+ * A value that is not finite spoils its own token only.
+ * post, pre: host structs holding device pointers.  One launch, no workspace.
+ * Errors: INVALID_ARG (NULL, n_tokens, d, k or copies < 1, an unknown type or kind, eps < 0, ld < d), LIMIT (n_tokens
+ * > 2^20, d > 32768, k or copies > 16), HIP.
+ */
+qmoe_status qmoe_residual_norm(const void *h /*device*/, int h_type, size_t ld_h, const void *y /*device or NULL*/,
+                               int y_type, size_t ld_y, int k, const float *gate /*device or NULL*/,
+                               const qmoe_norm *post /*host or NULL*/, float alpha,
+                               const float *channel_scale /*device or NULL*/, const qmoe_norm *pre /*host or NULL*/,
+                               void *h_out /*device or NULL*/, size_t ld_h_out, uint16_t *x_bf16 /*device or NULL*/,
+                               size_t ld_x, int copies, int n_tokens, int d, void *stream);
+
+/*
+ * The router's choice: k experts for every token from its logits, and their gates, in the form the layer
+ * calls take (expert_idx and gate of n_tokens * k rows, a token's k one after the other, best first).
+ *   key[e] = logits[t][e] + bias[e]   (one fp32 addition; bias NULL: the logit)
+ * The k largest keys are chosen, equal ones in the order of their index.  The bias takes part in the choice only:
+ *   QMOE_GATES_ALL     gate = exp(l) / sum of exp over all of the token's logits    (Switch: softmax, then top-k)
+ *   QMOE_GATES_CHOSEN  gate = exp(l) / sum of exp over its chosen logits            (gates of a token sum to 1)
+ * both with the largest logit of that sum subtracted first.  A logit of -infinity, or NaN, is masked: it has no share
+ * in a sum and is never chosen, nor is a key that is -infinity or NaN; +infinity counts as the largest finite number (so does
+ * a key that overflows).  Where fewer than k experts can be chosen the rest of the token's places get expert -1 and gate 0, which the layer calls
+ * answer with a zero row.  token_mask (device, one byte a token, 0 = padding; NULL = none): all k places of a
+ * masked token get -1 and 0; its logits are not read.
+ * ld: elements from a token's logits to the next one's, at least n_experts.
+ * One launch, no workspace.
+ * Errors: INVALID_ARG (NULL, a size < 1, k > n_experts, an unknown type or kind, ld < n_experts), LIMIT (n_experts > 16384, n_tokens > 2^20,
+ * k > 16), HIP.
+ */
+#define QMOE_GATES_ALL 0
+#define QMOE_GATES_CHOSEN 1
+qmoe_status qmoe_route(const void *logits /*device*/, int logits_type, size_t ld, const float *bias /*device or NULL*/,
+                       const uint8_t *token_mask /*device or NULL*/, int n_tokens, int n_experts, int k, int gates,
+                       int32_t *expert_idx /*device [n_tokens][k]*/, float *gate /*device [n_tokens][k]*/, void *stream);
+
+/* ------------------------------------------------------------------------- */
+/* Four-bit weights with a scale per group of columns                         */
+/* ------------------------------------------------------------------------- */
+
+/*
+ * For what ternary weights cost too much: the matrices that are not experts, layers that lose accuracy.
+ *   W[r][c] = s * (q[r][c] - z),  q in 0..15,  s = scale_f16[r][c / group],  z = zero[r][c / group] (0..15; no zeros: 8)
+ * A row is stored in blocks of 64 bytes = 128 columns (qmoe_int4_row_bytes): the 32-bit word 4 i + s of a block
+ * holds columns 32 s + 8 i .. 32 s + 8 i + 7 of it, column 2 j of these eight in bits 4 j .. 4 j + 3, column 2 j + 1 in
+ * bits 16 + 4 j .. 19 + 4 j (so the four words that a lane of a matrix-core operand needs for 128 columns are one
+ * 16-byte load, and a word becomes pairs of bf16 with a shift and a mask).  Columns past the last one of a row may hold anything.
+ */
+typedef struct qmoe_int4_matrix {
+    const uint8_t *weights;    /* device [rows][qmoe_int4_row_bytes(cols)], 16-byte aligned */
+    const uint16_t *scale_f16; /* device [rows][groups], groups = ceil(cols / group), finite */
+    const uint8_t *zero;       /* device [rows][groups], or NULL (= 8)                       */
+    int32_t rows, cols;
+    int32_t group;             /* columns that share a scale: 32, 64 or a multiple of 128    */
+    int32_t reserved;          /* 0 */
+} qmoe_int4_matrix;
+
+/* Bytes of a row of `cols` columns: 64 for every 128 columns begun; 0 if cols < 1. */
+size_t qmoe_int4_row_bytes(int cols);
+
+/*
+ * Values 0..15 (host, row-major [rows][cols]) to the stored form and back.  weights: host [rows][row bytes]; pack writes
+ * 0 in the columns past the last one.  Errors: INVALID_ARG, BAD_SYMBOL (a value above 15), LIMIT (rows > 2^24, cols > 2^20).
+ */
+qmoe_status qmoe_int4_pack_host(const uint8_t *values /*host*/, int rows, int cols, uint8_t *weights /*host*/);
+qmoe_status qmoe_int4_unpack_host(const uint8_t *weights /*host*/, int rows, int cols, uint8_t *values /*host*/);
+
+/*
+ * Round to nearest onto the grid (the simple quantiser; values from a better one go through qmoe_int4_pack_host).
+ * zero NULL: symmetric, s = fp16(max|w| / 7), q = clamp(round(w / s), -8, 7) + 8.  Else s = fp16((hi - lo) / 15) with
+ * lo = min(w, 0), hi = max(w, 0) over the group, z = clamp(round(-lo / s), 0, 15), q = clamp(round(w / s) + z, 0, 15).  A group whose s is
+ * 0 gets q = z (0 of it is kept exactly).  Rounding is to nearest even.
+ * Errors: INVALID_ARG (NULL, rows or cols < 1, a group that is none, a w that is not finite), LIMIT (rows > 2^24, cols > 2^20, a
+ * scale above the largest binary16).
+ */
+qmoe_status qmoe_int4_quantize_host(const float *w /*host [rows][cols]*/, int rows, int cols, int group,
+                                    uint8_t *weights /*host*/, uint16_t *scale_f16 /*host [rows][groups]*/,
+                                    uint8_t *zero /*host [rows][groups] or NULL*/);
+
+/*
+ * What follows a product.  The gated ones join two projections: the first rows / 2 rows of the matrix are the
+ * gate g, the others u, and the result has rows / 2 values: silu(g) * u = g / (1 + exp(-g)) * u, or gelu(g) * u with
+ * gelu(g) = g / 2 * (1 + tanh(sqrt(2 / pi) * (g + 0.044715 g^3))).
+ */
+#define QMOE_ACT_NONE 0
+#define QMOE_ACT_RELU 1
+#define QMOE_ACT_SILU_GATED 2
+#define QMOE_ACT_GELU_GATED 3
+
+/*
+ * One four-bit matrix times a batch of tokens, qmoe_decode_matvec's sibling:
+ *   y[b][r] = act( sum over groups of s * sum over the group's columns of (q - z) * x[b][c] ),  b < batch
+ * x: device bf16, ld_x elements from a token to the next (>= cols, any alignment that fits the type).  y: device fp32 or bf16
+ * (y_type), ld_y elements apart, overwritten; rows behind the last token and columns behind the last one are left as they were.
+ * Products are exact, sums fp32; a group's sum is scaled in fp32; one rounding at the end if y is bf16.
+ * An activation that is not finite spoils its own token only: every result of that token may be NaN.
+ * One launch, no workspace.
+ * Errors: INVALID_ARG (NULL, a size < 1, weights not 16-byte aligned, a group that is none, reserved not 0, an unknown type or
+ * activation, a gated one with odd rows, ld_x < cols, ld_y less than the results of a token), LIMIT (rows > 2^24, cols > 2^20, batch > 2^20), HIP.
+ */
+qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W /*host*/, const uint16_t *x_bf16 /*device*/, size_t ld_x, int batch,
+                             int activation, void *y /*device*/, int y_type, size_t ld_y, void *stream);
+
+/*
+ * qmoe_moe_layer_forward on experts in four bits:
+ *   y[t] = gate[t] * Wo[e] . bf16( act( Wi[e] . x[t] ) ),  e = expert_idx[t]
+ * wi, wo: device arrays [n_experts] of qmoe_int4_matrix (wi[e]: d_ff x d_model, with a gated activation 2 d_ff x d_model;
+ * wo[e]: d_model x d_ff), all with groups of `group` columns; the shapes in the descriptors are not read.  activation:
+ * QMOE_ACT_RELU or a gated one.  x: device bf16 [n_tokens][d_model], 16-byte aligned.  expert_idx, gate, tokens
+ * outside [0, n_experts), experts without tokens: as there.  y: device [n_tokens][d_model] fp32 or bf16 (y_type), 4-byte aligned,
+ * overwritten; apart from x, expert_idx and gate.  workspace: as there, qmoe_moe_layer_workspace(n_experts, d_model, d_ff, n_tokens) bytes.  An activation that is not
+ * finite spoils its own token only.
+ * Enqueues three kernels on `stream`: the dispatch and one per product; no second stream, no events.
+ * Calls that share a workspace must not overlap.
+ * Errors: INVALID_ARG (also d_model or d_ff not divisible by 8), WORKSPACE, LIMIT (as there; d_ff, d_model <= 32768), HIP.
+ */
+qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi /*device*/, const qmoe_int4_matrix *wo /*device*/, int group,
+                                    int activation, int n_experts, int d_model, int d_ff, const uint16_t *x_bf16 /*device*/,
+                                    const int32_t *expert_idx /*device*/, const float *gate /*device or NULL*/, int n_tokens,
+                                    void *y /*device*/, int y_type, void *workspace /*device*/, size_t workspace_bytes,
+                                    void *stream);
+
 /*
  * Launch tuning (process-wide, not thread-safe against running calls).  Keys:
  * "threads" (workgroup size of the scalar product kernel, a multiple of 64 up to 768),

@@ -12,4 +12,7 @@ from ._binding import (  # noqa: F401
     qmoe_moe_layer_ws_layout, qmoe_set_tuning, qmoe_stream_copy, qmoe_validate_host, qmoe_hook_set, qmoe_hook_several_lanes, qmoe_hook_rows_shares,
     qmoe_moe_layer_forward_static, qmoe_static_workspace_bytes, qmoe_lane_layout_build, qmoe_lane_layout_unpack,
     qmoe_plan_lanes, qmoe_plan_row_layout, format_lanes,
+    ACTIVATIONS, ACT_GELU_GATED, ACT_NONE, ACT_RELU, ACT_SILU_GATED, BF16, F32, GATES_ALL, GATES_CHOSEN, NORM_LAYER, NORM_RMS,
+    qmoe_int4_layer_forward, qmoe_int4_matrix, qmoe_int4_matvec, qmoe_int4_pack_host, qmoe_int4_quantize_host, qmoe_int4_row_bytes,
+    qmoe_int4_unpack_host, qmoe_norm, qmoe_residual_norm, qmoe_route,
 )

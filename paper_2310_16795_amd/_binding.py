@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_int, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_size_t, c_uint32, c_void_p
 
 import numpy as np
 
@@ -35,6 +35,24 @@ class qmoe_matrix(Structure):
 
 _MATRIX_BYTES = ctypes.sizeof(qmoe_matrix)
 
+
+class qmoe_norm(Structure):
+    _fields_ = [("kind", c_int32), ("eps", c_float), ("weight", c_void_p), ("bias", c_void_p)]
+
+
+class qmoe_int4_matrix(Structure):
+    _fields_ = [("weights", c_void_p), ("scale_f16", c_void_p), ("zero", c_void_p),
+                ("rows", c_int32), ("cols", c_int32), ("group", c_int32), ("reserved", c_int32)]
+
+
+_INT4_BYTES = ctypes.sizeof(qmoe_int4_matrix)
+
+F32, BF16 = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
+GATES_ALL, GATES_CHOSEN = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU_GATED, ACT_GELU_GATED = 0, 1, 2, 3
+ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU_GATED, "gelu": ACT_GELU_GATED}
+
 FORMAT_DEVICE_ORDER = 1
 FORMAT_GRID_MINMAX = 2
 
@@ -57,6 +75,8 @@ EXPORTS = [
     "qmoe_codes_to_device_order", "qmoe_decompress", "qmoe_encode_device", "qmoe_hook_set", "qmoe_static_workspace_bytes", "qmoe_moe_layer_forward_static",
     "qmoe_lane_layout_size", "qmoe_lane_layout_build", "qmoe_lane_layout_unpack", "qmoe_plan_lanes",
     "qmoe_plan_row_layout", "qmoe_hook_several_lanes", "qmoe_hook_rows_shares",
+    "qmoe_residual_norm", "qmoe_route", "qmoe_int4_row_bytes", "qmoe_int4_pack_host", "qmoe_int4_unpack_host",
+    "qmoe_int4_quantize_host", "qmoe_int4_matvec", "qmoe_int4_layer_forward",
 ]
 
 
@@ -110,6 +130,18 @@ def lib():
         L.qmoe_hook_several_lanes.argtypes = [vp, i, i, i, i, i]
         L.qmoe_hook_rows_shares.argtypes = [i, vp, i, i, vp]
         L.qmoe_stream_copy.argtypes = [vp, vp, sz, vp]
+        operators = {
+            "qmoe_residual_norm": [vp, i, sz, vp, i, sz, i, vp, vp, c_float, vp, vp, vp, sz, vp, sz, i, i, i, vp],
+            "qmoe_route": [vp, i, sz, vp, vp, i, i, i, i, vp, vp, vp],
+            "qmoe_int4_row_bytes": [i], "qmoe_int4_pack_host": [vp, i, i, vp], "qmoe_int4_unpack_host": [vp, i, i, vp],
+            "qmoe_int4_quantize_host": [vp, i, i, i, vp, vp, vp],
+            "qmoe_int4_matvec": [vp, vp, sz, i, i, vp, i, sz, vp],
+            "qmoe_int4_layer_forward": [vp, vp, i, i, i, i, i, vp, vp, vp, i, vp, i, vp, sz, vp],
+        }
+        for name, args in operators.items():  # (a library that QMOE_LIBRARY names may be built without their units)
+            if hasattr(L, name):
+                getattr(L, name).argtypes = args
+                getattr(L, name).restype = sz if name == "qmoe_int4_row_bytes" else i
         _lib = L
     return _lib
 
@@ -341,6 +373,153 @@ def qmoe_bf16_layer_forward(wi_ptrs, wo_ptrs, n_experts: int, d_model: int, d_ff
                                          _dev_ptr(y), _dev_ptr(workspace),
                                          workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
            "qmoe_bf16_layer_forward")
+
+
+# ------------------------------------------------------------------ around the layer
+
+def _type_of(t, what: str) -> int:
+    """QMOE_F32 or QMOE_BF16 of a tensor (16-bit integers stand for bf16 bits)."""
+    import torch
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype in (torch.bfloat16, torch.int16) or t.dtype == getattr(torch, "uint16", None):
+        return BF16
+    raise ValueError(f"{what} must be float32 or bfloat16")
+
+
+def _rows_ptr(t, what: str) -> int:
+    """Address of a device matrix whose rows are contiguous, any number of elements apart."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{what} must be a matrix of contiguous rows")
+    return t.data_ptr()
+
+
+def _row_stride(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _vector(t, n: int, what: str) -> int:
+    """Address of a contiguous device float32 array of n values (None -> NULL)."""
+    import torch
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.numel() != n:
+        raise ValueError(f"{what} must be float32 with {n} values")
+    return _dev_ptr(t)
+
+
+def _norm_ptr(n, d: int, what: str):
+    """n: qmoe_norm, an object with one in .desc and its width in .d (device.DeviceNorm), or None."""
+    if n is None:
+        return None
+    if getattr(n, "d", d) not in (None, d):
+        raise ValueError(f"{what} is a norm of {n.d} values, not {d}")
+    return byref(getattr(n, "desc", n))
+
+
+def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, post=None, alpha: float = 1.0, channel_scale=None,
+                       pre=None, copies: int = 1, stream=None) -> None:
+    """h, h_out: device [n, d] float32 or bfloat16 (h_out may be h); y: [n * k, d] float32 or bfloat16; x: [n * copies, d] bfloat16;
+    gate: float32, n * k values; channel_scale: float32 [d]; post, pre: device.DeviceNorm."""
+    n, d = h.shape
+    if y is not None and tuple(y.shape) != (n * k, d) or h_out is not None and (h_out.shape != h.shape or h_out.dtype != h.dtype) or \
+            x is not None and tuple(x.shape) != (n * copies, d):
+        raise ValueError("shape mismatch")
+    if x is not None and _type_of(x, "x") != BF16:
+        raise ValueError("x must be bfloat16")
+    _check(lib().qmoe_residual_norm(
+        _rows_ptr(h, "h"), _type_of(h, "h"), _row_stride(h), 0 if y is None else _rows_ptr(y, "y"), 0 if y is None else _type_of(y, "y"),
+        0 if y is None else _row_stride(y), k, _vector(gate, n * k, "gate"), _norm_ptr(post, d, "post"), alpha,
+        _vector(channel_scale, d, "channel_scale"), _norm_ptr(pre, d, "pre"), 0 if h_out is None else _rows_ptr(h_out, "h_out"),
+        0 if h_out is None else _row_stride(h_out), 0 if x is None else _rows_ptr(x, "x"), 0 if x is None else _row_stride(x),
+        copies, n, d, _stream_ptr(stream)), "qmoe_residual_norm")
+
+
+def qmoe_route(logits, expert_idx, gate, bias=None, token_mask=None, gates: int = GATES_ALL, stream=None) -> None:
+    """logits: device [n, n_experts] float32 or bfloat16; expert_idx: int32 [n, k]; gate: float32 [n, k]; bias: float32
+    [n_experts]; token_mask: one byte (or bool) a token, 0 = padding."""
+    import torch
+    n, n_experts = logits.shape
+    k = expert_idx.shape[1]
+    if tuple(expert_idx.shape) != (n, k) or tuple(gate.shape) != (n, k):
+        raise ValueError("shape mismatch")
+    if expert_idx.dtype != torch.int32 or gate.dtype != torch.float32:
+        raise ValueError("expert_idx must be int32, gate float32")
+    if token_mask is not None and (token_mask.numel() != n or token_mask.element_size() != 1):
+        raise ValueError("token_mask must hold a byte for every token")
+    _check(lib().qmoe_route(_rows_ptr(logits, "logits"), _type_of(logits, "logits"), _row_stride(logits),
+                            _vector(bias, n_experts, "bias"), _dev_ptr(token_mask), n, n_experts, k, gates, _dev_ptr(expert_idx),
+                            _dev_ptr(gate), _stream_ptr(stream)), "qmoe_route")
+
+
+# ------------------------------------------------------------------ four-bit weights
+
+def qmoe_int4_row_bytes(cols: int) -> int:
+    return lib().qmoe_int4_row_bytes(cols)
+
+
+def qmoe_int4_pack_host(values: np.ndarray) -> np.ndarray:
+    """uint8 [rows, cols] of 0..15 -> the stored form, uint8 [rows, row bytes]"""
+    v = np.ascontiguousarray(values, dtype=np.uint8)
+    if v.ndim != 2:
+        raise ValueError("2-D matrix expected")
+    out = np.empty((v.shape[0], qmoe_int4_row_bytes(v.shape[1])), dtype=np.uint8)
+    _check(lib().qmoe_int4_pack_host(_host_ptr(v), v.shape[0], v.shape[1], _host_ptr(out)), "qmoe_int4_pack_host")
+    return out
+
+
+def qmoe_int4_unpack_host(weights: np.ndarray, cols: int) -> np.ndarray:
+    """The stored form -> uint8 [rows, cols] of 0..15"""
+    w = np.ascontiguousarray(weights, dtype=np.uint8)
+    if w.ndim != 2 or w.shape[1] != qmoe_int4_row_bytes(cols):
+        raise ValueError("rows of qmoe_int4_row_bytes(cols) bytes expected")
+    out = np.empty((w.shape[0], cols), dtype=np.uint8)
+    _check(lib().qmoe_int4_unpack_host(_host_ptr(w), w.shape[0], cols, _host_ptr(out)), "qmoe_int4_unpack_host")
+    return out
+
+
+def qmoe_int4_quantize_host(w: np.ndarray, group: int = 128, zero: bool = False):
+    """float32 [rows, cols] -> (weights uint8 [rows, row bytes], scale_f16 uint16 [rows, groups], zero uint8 [rows, groups] or None)"""
+    v = np.ascontiguousarray(w, dtype=np.float32)
+    if v.ndim != 2 or group < 1:
+        raise ValueError("2-D matrix and a positive group expected")
+    rows, cols = v.shape
+    groups = (cols + group - 1) // group
+    out, scale = np.empty((rows, qmoe_int4_row_bytes(cols)), dtype=np.uint8), np.empty((rows, groups), dtype=np.uint16)
+    z = np.empty((rows, groups), dtype=np.uint8) if zero else None
+    _check(lib().qmoe_int4_quantize_host(_host_ptr(v), rows, cols, group, _host_ptr(out), _host_ptr(scale),
+                                         None if z is None else _host_ptr(z)), "qmoe_int4_quantize_host")
+    return out, scale, z
+
+
+def qmoe_int4_matvec(W: qmoe_int4_matrix, x_bf16, y, activation: int = ACT_NONE, stream=None) -> None:
+    """x_bf16: device bfloat16 [batch, cols]; y: device float32 or bfloat16 [batch, rows] (gated activations: rows / 2)."""
+    batch, cols = x_bf16.shape
+    if cols != W.cols or tuple(y.shape) != (batch, W.rows // 2 if activation >= ACT_SILU_GATED else W.rows):
+        raise ValueError("shape mismatch")
+    if _type_of(x_bf16, "x") != BF16:
+        raise ValueError("x must be bfloat16")
+    _check(lib().qmoe_int4_matvec(byref(W), _rows_ptr(x_bf16, "x"), _row_stride(x_bf16), batch, activation, _rows_ptr(y, "y"),
+                                  _type_of(y, "y"), _row_stride(y), _stream_ptr(stream)), "qmoe_int4_matvec")
+
+
+def qmoe_int4_layer_forward(wi_dev, wo_dev, group: int, activation: int, n_experts: int, d_model: int, d_ff: int, x_bf16, expert_idx,
+                            gate, y, workspace, stream=None) -> None:
+    """wi_dev / wo_dev: device byte tensors holding n_experts qmoe_int4_matrix structs; y: float32 or bfloat16."""
+    n_tokens = x_bf16.shape[0]
+    if tuple(x_bf16.shape) != (n_tokens, d_model) or tuple(y.shape) != (n_tokens, d_model) or expert_idx.numel() != n_tokens:
+        raise ValueError("shape mismatch")
+    if _type_of(x_bf16, "x") != BF16 or expert_idx.element_size() != 4:
+        raise ValueError("x must be bfloat16, expert_idx int32")
+    if min(t.numel() * t.element_size() for t in (wi_dev, wo_dev)) < _INT4_BYTES * n_experts:
+        raise ValueError("expert descriptor arrays too small")
+    _check(lib().qmoe_int4_layer_forward(_dev_ptr(wi_dev), _dev_ptr(wo_dev), group, activation, n_experts, d_model, d_ff,
+                                         _dev_ptr(x_bf16), _dev_ptr(expert_idx), _vector(gate, n_tokens, "gate"), n_tokens,
+                                         _dev_ptr(y), _type_of(y, "y"), _dev_ptr(workspace),
+                                         workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "qmoe_int4_layer_forward")
 
 
 def qmoe_set_tuning(key: str, value: int) -> None:

@@ -3,6 +3,7 @@
 
 #include "qmoe_dev.h"
 #include "qmoe_encode.h"
+#include "qmoe_ops.h"
 
 namespace qmoe {
 
@@ -614,6 +615,36 @@ qmoe_status launch_dispatch(const DispatchArgs &da, hipStream_t s)
     return st != QMOE_OK ? st : launch_dispatch_kernel(da, di.max_lds, s);
 }
 }  // namespace
+
+// ---- for the operators around the ternary layer (qmoe_ops.h)
+qmoe_status gpu_info(DeviceInfo *out) { return device_info(out); }
+
+qmoe_status layer_workspace_ok(int n_tokens, int n_experts, int d_model, int d_ff, const void *workspace, size_t workspace_bytes)
+{
+    qmoe_ws_layout l;
+    const qmoe_status st = qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens, &l);
+    if (st != QMOE_OK) return st;
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < l.total - kShareRecords)
+        return QMOE_E_WORKSPACE;
+    return QMOE_OK;
+}
+
+qmoe_status group_by_expert(const int32_t *expert_idx, int n_tokens, int n_experts, int d_model, int d_ff, void *workspace, float *y,
+                            int row_words, hipStream_t s, GroupedTokens *out)
+{
+    qmoe_ws_layout l;
+    const qmoe_status st = qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens, &l);
+    if (st != QMOE_OK) return st;
+    const LayerPtrs lp = layer_ptrs(workspace, l);
+    MmPlan all;  // every expert's tokens in tiles of kMmTokens
+    all.min_tokens = all.otherwise = 1;
+    out->items = lp.items_mm;
+    out->n_items = lp.counters + kCounterMm;
+    out->perm = lp.perm;
+    out->hidden = lp.hidden;
+    out->max_items = n_tokens;
+    return launch_dispatch(dispatch_args(expert_idx, n_tokens, n_experts, row_words, lp, 4, 4, all, y), s);
+}
 }  // namespace qmoe
 
 using namespace qmoe;

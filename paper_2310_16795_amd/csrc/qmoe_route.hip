@@ -1,0 +1,246 @@
+// qmoe_route: the experts of every token and their gates, from the router's logits.
+#include <cfloat>
+
+#include "qmoe_ops.h"
+
+namespace qmoe {
+namespace {
+
+struct RouteArgs {
+    const void *logits;
+    size_t ld;
+    const float *bias;
+    const uint8_t *mask;
+    int *idx;
+    float *gate;
+    int n_tokens, n_experts, k, chosen;
+};
+
+// A logit as the operator counts it: masked (-infinity) if it is NaN, finite if it is +infinity.
+__device__ __forceinline__ float counted(float l) { return l == l ? fminf(l, FLT_MAX) : -INFINITY; }
+__device__ __forceinline__ float key_of(float l, float bias) { return l == -INFINITY ? l : counted(l + bias); }
+
+template <int TYPE>
+__device__ __forceinline__ float logit(const void *base, size_t at)
+{
+    if constexpr (TYPE == QMOE_F32) return static_cast<const float *>(base)[at];
+    else return bf16_bits_to_float(static_cast<const uint16_t *>(base)[at]);
+}
+
+// Over the LANES lanes (16: a row of the wavefront; 64: all of it) that share a token, in every one of them.
+template <int LANES, typename F>
+__device__ __forceinline__ float over_lanes(float x, F f)
+{
+    x = f(x, dpp_f<0x121, 0xf>(x, x));
+    x = f(x, dpp_f<0x122, 0xf>(x, x));
+    x = f(x, dpp_f<0x124, 0xf>(x, x));
+    x = f(x, dpp_f<0x128, 0xf>(x, x));
+    if constexpr (LANES == 64) {
+        const float a = f(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 15)),
+                          __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 31)));
+        const float b = f(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 47)),
+                          __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)));
+        x = f(a, b);
+    }
+    return x;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float x)
+{
+    return over_lanes<LANES>(x, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x)
+{
+    return over_lanes<LANES>(x, [](float a, float b) { return a + b; });
+}
+template <int LANES>
+__device__ __forceinline__ int lanes_min(int x)
+{
+    auto step = [&](auto ctrl) {
+        constexpr int c = decltype(ctrl)::value;
+        x = min(x, __builtin_amdgcn_update_dpp(x, x, c, 0xf, 0xf, false));
+    };
+    step(std::integral_constant<int, 0x121>{});
+    step(std::integral_constant<int, 0x122>{});
+    step(std::integral_constant<int, 0x124>{});
+    step(std::integral_constant<int, 0x128>{});
+    if constexpr (LANES == 64)
+        x = min(min(__builtin_amdgcn_readlane(x, 15), __builtin_amdgcn_readlane(x, 31)),
+                min(__builtin_amdgcn_readlane(x, 47), __builtin_amdgcn_readlane(x, 63)));
+    return x;
+}
+
+// The gates of the experts that the token's first k lanes hold (mine, -1 = none), and what the call returns of them.
+template <int TYPE, int LANES>
+__device__ __forceinline__ void finish(const RouteArgs &a, int t, int l, int mine, float top, float sum)
+{
+    float v = -INFINITY;
+    if (l < a.k && mine >= 0) v = counted(logit<TYPE>(a.logits, (size_t)t * a.ld + mine));
+    if (a.chosen) {
+        top = lanes_max<LANES>(v);
+        sum = lanes_sum<LANES>(v == -INFINITY ? 0.0f : expf(v - top));
+    }
+    if (l < a.k) {
+        a.idx[(size_t)t * a.k + l] = mine;
+        a.gate[(size_t)t * a.k + l] = mine >= 0 ? expf(v - top) / sum : 0.0f;
+    }
+}
+
+// A token's keys lie in the registers of LANES lanes, expert l + LANES * i in lane l's register i: one pass over memory.
+// Each of the k rounds takes the largest key (a reduction over the lanes), of equal ones that of the lowest index (a
+// second one), and the lane that held it looks for its next best.
+template <int TYPE, int LANES, int PER, bool BIAS>
+__global__ __launch_bounds__(256) void k_route(const RouteArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (LANES - 1);
+    const int per_wave = 64 / LANES;
+    const int t = (int)(blockIdx.x * 4 + wave) * per_wave + lane / LANES;
+    const bool there = t < a.n_tokens && !(a.mask && a.mask[t] == 0);
+    float key[PER];
+    float top = 0.0f, sum = 0.0f;
+    {
+        float v[PER];
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int e = l + LANES * i;
+            v[i] = -INFINITY;
+            if (there && e < a.n_experts) v[i] = logit<TYPE>(a.logits, (size_t)t * a.ld + e);
+        }
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int i = 0; i < PER; i++) {
+                const int e = l + LANES * i;
+                key[i] = e < a.n_experts ? a.bias[e] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            v[i] = counted(v[i]);
+            key[i] = BIAS ? key_of(v[i], key[i]) : v[i];
+        }
+        if (!a.chosen) {
+            top = v[0];
+#pragma unroll
+            for (int i = 1; i < PER; i++) top = fmaxf(top, v[i]);
+            top = lanes_max<LANES>(top);
+#pragma unroll
+            for (int i = 0; i < PER; i++) sum += v[i] == -INFINITY ? 0.0f : expf(v[i] - top);
+            sum = lanes_sum<LANES>(sum);
+        }
+    }
+    float best = key[0];
+    int best_i = 0;
+#pragma unroll
+    for (int i = 1; i < PER; i++)
+        if (key[i] > best) best = key[i], best_i = i;
+    int mine = -1;
+    for (int j = 0; j < a.k; j++) {
+        const float m = lanes_max<LANES>(best);
+        const int e = lanes_min<LANES>(best == m ? l + LANES * best_i : 0x7FFFFFFF);
+        if (l == j) mine = m == -INFINITY ? -1 : e;
+        if (e == l + LANES * best_i) {  // one lane of the token's
+            best = -INFINITY;
+            const int gone = best_i;
+#pragma unroll
+            for (int i = 0; i < PER; i++) {
+                if (i == gone) key[i] = -INFINITY;
+                if (key[i] > best) best = key[i], best_i = i;
+            }
+        }
+    }
+    if (t < a.n_tokens) finish<TYPE, LANES>(a, t, l, mine, top, sum);
+}
+
+// More experts than registers hold: a workgroup a token, the logits read again for every round (from L2 as a rule): the
+// largest key behind the last one taken, in the order (key down, index up).
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_route_wide(const RouteArgs a)
+{
+    __shared__ float s_val[4];
+    __shared__ int s_idx[4];
+    const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool there = !(a.mask && a.mask[t] == 0);
+    auto all_max = [&](float v) {
+        v = lanes_max<64>(v);
+        __syncthreads();
+        if (lane == 0) s_val[wave] = v;
+        __syncthreads();
+        return fmaxf(fmaxf(s_val[0], s_val[1]), fmaxf(s_val[2], s_val[3]));
+    };
+    float top = 0.0f, sum = 0.0f;
+    const size_t row = (size_t)t * a.ld;
+    if (there && !a.chosen) {
+        top = -INFINITY;
+        for (int e = threadIdx.x; e < a.n_experts; e += 256) top = fmaxf(top, counted(logit<TYPE>(a.logits, row + e)));
+        top = all_max(top);
+        for (int e = threadIdx.x; e < a.n_experts; e += 256) {
+            const float v = counted(logit<TYPE>(a.logits, row + e));
+            sum += v == -INFINITY ? 0.0f : expf(v - top);
+        }
+        sum = lanes_sum<64>(sum);
+        __syncthreads();
+        if (lane == 0) s_val[wave] = sum;
+        __syncthreads();
+        sum = (s_val[0] + s_val[1]) + (s_val[2] + s_val[3]);
+    }
+    float last = INFINITY;
+    int last_e = -1, mine = -1;
+    for (int j = 0; there && j < a.k; j++) {
+        float best = -INFINITY;
+        int best_e = 0x7FFFFFFF;
+        for (int e = threadIdx.x; e < a.n_experts; e += 256) {
+            const float v = key_of(counted(logit<TYPE>(a.logits, row + e)), a.bias ? a.bias[e] : 0.0f);
+            if ((v < last || (v == last && e > last_e)) && v > best) best = v, best_e = e;
+        }
+        const float m = all_max(best);
+        const int e = lanes_min<64>(best == m ? best_e : 0x7FFFFFFF);
+        if (lane == 0) s_idx[wave] = e;
+        __syncthreads();
+        last = m;
+        last_e = min(min(s_idx[0], s_idx[1]), min(s_idx[2], s_idx[3]));
+        if (m == -INFINITY) break;  // the same for the whole workgroup
+        if (lane == j) mine = last_e;
+    }
+    if (wave == 0) finish<TYPE, 64>(a, t, lane, mine, top, sum);
+}
+
+template <int TYPE, int LANES, int PER>
+void launch_per(const RouteArgs &a, hipStream_t s)
+{
+    const int a_block = 4 * (64 / LANES), grid = (a.n_tokens + a_block - 1) / a_block;
+    if (a.bias) hipLaunchKernelGGL((k_route<TYPE, LANES, PER, true>), dim3(grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_route<TYPE, LANES, PER, false>), dim3(grid), dim3(256), 0, s, a);
+}
+
+template <int TYPE>
+qmoe_status launch_route(const RouteArgs &a, hipStream_t s)
+{
+    const int e = a.n_experts;
+    if (e <= 64) launch_per<TYPE, 16, 4>(a, s);
+    else if (e <= 128) launch_per<TYPE, 16, 8>(a, s);
+    else if (e <= 256) launch_per<TYPE, 16, 16>(a, s);
+    else if (e <= 512) launch_per<TYPE, 64, 8>(a, s);
+    else if (e <= 1024) launch_per<TYPE, 64, 16>(a, s);
+    else if (e <= 2048) launch_per<TYPE, 64, 32>(a, s);
+    else hipLaunchKernelGGL((k_route_wide<TYPE>), dim3(a.n_tokens), dim3(256), 0, s, a);
+    QMOE_HIP_TRY(hipGetLastError());
+    return QMOE_OK;
+}
+
+}  // namespace
+}  // namespace qmoe
+
+using namespace qmoe;
+
+extern "C" qmoe_status qmoe_route(const void *logits, int logits_type, size_t ld, const float *bias, const uint8_t *token_mask,
+                                  int n_tokens, int n_experts, int k, int gates, int32_t *expert_idx, float *gate, void *stream)
+{
+    if (!logits || !expert_idx || !gate || n_tokens < 1 || n_experts < 1 || k < 1 || k > n_experts || ld < (size_t)n_experts ||
+        (logits_type != QMOE_F32 && logits_type != QMOE_BF16) || (gates != QMOE_GATES_ALL && gates != QMOE_GATES_CHOSEN))
+        return QMOE_E_INVALID_ARG;
+    if (n_experts > kMaxExperts || n_tokens > kMaxTokens || k > kMaxJoined) return QMOE_E_LIMIT;
+    const RouteArgs a{logits, ld, bias, token_mask, expert_idx, gate, n_tokens, n_experts, k, gates == QMOE_GATES_CHOSEN};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return logits_type == QMOE_F32 ? launch_route<QMOE_F32>(a, s) : launch_route<QMOE_BF16>(a, s);
+}

@@ -167,6 +167,68 @@ class DeviceLayer:
                                         self.n_experts, self.d_model, self.d_ff, x_bf16, expert_idx, gate, y, stream)
 
 
+class DeviceNorm:
+    """A norm's descriptor beside its weight and bias (device float32 [d], or None)."""
+
+    KINDS = {"rms": B.NORM_RMS, "layer": B.NORM_LAYER}
+
+    def __init__(self, kind: str, weight: "torch.Tensor | None" = None, bias: "torch.Tensor | None" = None, eps: float = 1e-6):
+        given = [t for t in (weight, bias) if t is not None]
+        if any(t.dtype != torch.float32 or t.dim() != 1 or t.numel() != given[0].numel() for t in given):
+            raise ValueError("weight and bias must be float32 vectors of one width")
+        self.weight, self.bias, self.d = weight, bias, given[0].numel() if given else None
+        self.desc = B.qmoe_norm(self.KINDS[kind], eps, *(B._dev_ptr(t) or None for t in (weight, bias)))
+
+
+def _int4_shapes(weights: torch.Tensor, scale: torch.Tensor, zero: "torch.Tensor | None", lead: tuple, cols: int, group: int):
+    groups = (cols + group - 1) // group
+    if weights.dtype != torch.uint8 or tuple(weights.shape) != (*lead, B.qmoe_int4_row_bytes(cols)):
+        raise ValueError("weights must be uint8 [..., rows, row bytes]")
+    if scale.element_size() != 2 or tuple(scale.shape) != (*lead, groups):
+        raise ValueError("scale must be 16-bit [..., rows, groups]")
+    if zero is not None and (zero.dtype != torch.uint8 or zero.shape != scale.shape):
+        raise ValueError("zero must be uint8 [..., rows, groups]")
+
+
+class DeviceInt4Matrix:
+    """One four-bit matrix in device memory and its qmoe_int4_matrix descriptor."""
+
+    def __init__(self, weights: torch.Tensor, scale: torch.Tensor, cols: int, group: int, zero: "torch.Tensor | None" = None):
+        """weights: uint8 [rows, row bytes]; scale: binary16 [rows, groups]; zero: uint8 [rows, groups] or None (= 8)."""
+        rows = weights.shape[0]
+        _int4_shapes(weights, scale, zero, (rows,), cols, group)
+        self.weights, self.scale, self.zero = weights, scale, zero
+        self.desc = B.qmoe_int4_matrix(B._dev_ptr(weights), B._dev_ptr(scale), B._dev_ptr(zero) or None, rows, cols, group, 0)
+
+
+class DeviceInt4Layer:
+    """All experts of one layer in four bits: stacked device tensors and the arrays of descriptors that point into them."""
+
+    def __init__(self, wi, wo, d_model: int, d_ff: int, group: int, activation: str = "relu"):
+        """wi, wo: (weights uint8 [n_experts, rows, row bytes], scale binary16 [n_experts, rows, groups], zero uint8 like scale or None);
+        rows of wi: d_ff, with a gated activation ("silu", "gelu") 2 * d_ff, the gate's first."""
+        self.n_experts, self.d_model, self.d_ff, self.group = wi[0].shape[0], d_model, d_ff, group
+        self.activation = B.ACTIVATIONS[activation]
+        self.device = wi[0].device
+        self.tensors, self.desc_dev = (tuple(wi), tuple(wo)), []
+        rows_wi = d_ff if self.activation == B.ACT_RELU else 2 * d_ff
+        for (w, s, z), rows, cols in ((wi, rows_wi, d_model), (wo, d_model, d_ff)):
+            _int4_shapes(w, s, z, (self.n_experts, rows), cols, group)
+            at = [(B._dev_ptr(t), t[0].numel() * t.element_size()) if t is not None else (0, 0) for t in (w, s, z)]
+            descs = (B.qmoe_int4_matrix * self.n_experts)(*[
+                B.qmoe_int4_matrix(*(p + e * n or None for p, n in at), rows, cols, group, 0) for e in range(self.n_experts)])
+            self.desc_dev.append(torch.from_numpy(np.frombuffer(bytes(descs), dtype=np.uint8).copy()).to(self.device))
+
+    def workspace(self, n_tokens: int) -> torch.Tensor:
+        n = B.qmoe_moe_layer_workspace(self.n_experts, self.d_model, self.d_ff, n_tokens)
+        return torch.empty(n, dtype=torch.uint8, device=self.device)
+
+    def forward(self, x_bf16: torch.Tensor, expert_idx: torch.Tensor, y: torch.Tensor, workspace: torch.Tensor,
+                gate: "torch.Tensor | None" = None, stream=None):
+        B.qmoe_int4_layer_forward(*self.desc_dev, self.group, self.activation, self.n_experts, self.d_model, self.d_ff, x_bf16,
+                                  expert_idx, gate, y, workspace, stream)
+
+
 def read_workspace(workspace: torch.Tensor, n_experts: int, d_model: int, d_ff: int, n_tokens: int):
     """Copy the dispatch results out of a layer workspace (synchronises)."""
     l = B.qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens)
