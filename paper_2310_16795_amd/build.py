@@ -19,10 +19,12 @@ OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(CSRC, "libqmoe.so")
 UNITS = ["qmoe_host.cpp", "qmoe_api.hip", "qmoe_product_sym.hip", "qmoe_product_asym.hip", "qmoe_product_mm.hip",
          "qmoe_rows.hip", "qmoe_decompress.hip", "qmoe_matvec.hip", "qmoe_dispatch.hip", "qmoe_encode.hip", "qmoe_misc.hip",
-         "qmoe_norm.hip", "qmoe_route.hip", "qmoe_int4.hip", "qmoe_int4_host.cpp"]
+         "qmoe_norm.hip", "qmoe_route.hip", "qmoe_int4.hip", "qmoe_int4_mm_plain.hip", "qmoe_int4_mm_zeros.hip",
+         "qmoe_int4_mm_gated.hip", "qmoe_int4_mm_gated_zeros.hip", "qmoe_int4_host.cpp"]
 HEADERS = [os.path.join(ROOT, "include", "qmoe.h"), os.path.join(ROOT, "include", "qmoe_hooks.h"),
            os.path.join(CSRC, "qmoe_internal.h"), os.path.join(CSRC, "qmoe_dev.h"), os.path.join(CSRC, "qmoe_product.h"),
-           os.path.join(CSRC, "qmoe_encode.h"), os.path.join(CSRC, "qmoe_ops.h"), os.path.join(CSRC, "qmoe_int4.h")]
+           os.path.join(CSRC, "qmoe_encode.h"), os.path.join(CSRC, "qmoe_ops.h"), os.path.join(CSRC, "qmoe_int4.h"),
+           os.path.join(CSRC, "qmoe_int4_mm.h")]
 SOURCES = [os.path.join(CSRC, u) for u in UNITS]
 
 FLAGS = [

@@ -62,6 +62,8 @@ __device__ __forceinline__ u32x4 int4_x(const uint16_t *row, int c, int cols)
     return v;
 }
 
+inline bool int4_is_gated(int activation) { return activation == QMOE_ACT_SILU_GATED || activation == QMOE_ACT_GELU_GATED; }
+
 __device__ __forceinline__ float int4_gated(float g, float u, int activation)
 {
     if (activation == QMOE_ACT_SILU_GATED) return g / (1.0f + expf(-g)) * u;
@@ -76,5 +78,11 @@ __device__ __forceinline__ void int4_store(const Int4Args &a, size_t out_row, fl
     if (a.out_f32) static_cast<float *>(a.out)[at] = v;
     else static_cast<uint16_t *>(a.out)[at] = bf16_bits(v);
 }
+
+// qmoe_int4_mm_*.hip
+qmoe_status launch_int4_mm_plain(const Int4Args &a, int cus, hipStream_t s);
+qmoe_status launch_int4_mm_zeros(const Int4Args &a, int cus, hipStream_t s);
+qmoe_status launch_int4_mm_gated(const Int4Args &a, int cus, hipStream_t s);
+qmoe_status launch_int4_mm_gated_zeros(const Int4Args &a, int cus, hipStream_t s);
 
 }  // namespace qmoe

@@ -153,8 +153,6 @@ __global__ __launch_bounds__(512) void k_int4_rows(const Int4Args a)
     }
 }
 
-bool gated(int activation) { return activation == QMOE_ACT_SILU_GATED || activation == QMOE_ACT_GELU_GATED; }
-
 bool group_ok(int group) { return group == 32 || group == 64 || (group > 0 && group % kInt4BlockCols == 0); }
 
 // rows: results a token
@@ -171,8 +169,8 @@ void fill_shape(Int4Args *a, int rows, int cols, int group)
 template <int TILES>
 qmoe_status launch_tiles(const Int4Args &a, int grid, int threads, hipStream_t s)
 {
-    const size_t smem = a.split > 1 ? (size_t)(threads / 64) * (gated(a.activation) ? 2 : 1) * TILES * 64 * sizeof(f32x4) : 0;
-    if (gated(a.activation)) {
+    const size_t smem = a.split > 1 ? (size_t)(threads / 64) * (int4_is_gated(a.activation) ? 2 : 1) * TILES * 64 * sizeof(f32x4) : 0;
+    if (int4_is_gated(a.activation)) {
         const qmoe_status st = allow_lds(k_int4_rows<TILES, true>, smem);
         if (st != QMOE_OK) return st;
         hipLaunchKernelGGL((k_int4_rows<TILES, true>), dim3(grid), dim3(threads), smem, s, a);
@@ -200,6 +198,13 @@ qmoe_status launch_rows_kernel(Int4Args a, int tiles, long long items, int cus, 
     return launch_tiles<4>(a, grid, threads, s);
 }
 
+// zeros: a matrix has zero points (descriptors in device memory: may have)
+qmoe_status launch_mm_kernel(const Int4Args &a, bool zeros, int cus, hipStream_t s)
+{
+    if (int4_is_gated(a.activation)) return zeros ? launch_int4_mm_gated_zeros(a, cus, s) : launch_int4_mm_gated(a, cus, s);
+    return zeros ? launch_int4_mm_zeros(a, cus, s) : launch_int4_mm_plain(a, cus, s);
+}
+
 }  // namespace
 }  // namespace qmoe
 
@@ -212,9 +217,9 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W, const uint16_t *x_bf16, 
 {
     if (!W || !W->weights || !W->scale_f16 || !x_bf16 || !y || W->rows < 1 || W->cols < 1 || batch < 1 || !group_ok(W->group) ||
         W->reserved || reinterpret_cast<uintptr_t>(W->weights) % 16 || (y_type != QMOE_F32 && y_type != QMOE_BF16) ||
-        activation < QMOE_ACT_NONE || activation > QMOE_ACT_GELU_GATED || (gated(activation) && W->rows % 2))
+        activation < QMOE_ACT_NONE || activation > QMOE_ACT_GELU_GATED || (int4_is_gated(activation) && W->rows % 2))
         return QMOE_E_INVALID_ARG;
-    const int rows = gated(activation) ? W->rows / 2 : W->rows;
+    const int rows = int4_is_gated(activation) ? W->rows / 2 : W->rows;
     if (ld_x < (size_t)W->cols || ld_y < (size_t)rows) return QMOE_E_INVALID_ARG;
     if (W->rows > kMaxInt4Rows || W->cols > kMaxInt4Cols || batch > kMaxTokens) return QMOE_E_LIMIT;
     DeviceInfo di;
@@ -232,6 +237,7 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W, const uint16_t *x_bf16, 
     a.out_f32 = y_type == QMOE_F32;
     a.activation = activation;
     fill_shape(&a, rows, W->cols, W->group);
+    if (batch > 64) return launch_mm_kernel(a, a.zero != nullptr, di.cus, static_cast<hipStream_t>(stream));
     const int tiles = (batch + 15) / 16, at_once = tiles <= 2 ? tiles : 4;
     return launch_rows_kernel(a, tiles, (tiles + at_once - 1) / at_once, di.cus, static_cast<hipStream_t>(stream));
 }
@@ -240,7 +246,7 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
                                     int d_model, int d_ff, const uint16_t *x_bf16, const int32_t *expert_idx, const float *gate,
                                     int n_tokens, void *y, int y_type, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!wi || !wo || !x_bf16 || !expert_idx || !y || !group_ok(group) || (activation != QMOE_ACT_RELU && !gated(activation)) ||
+    if (!wi || !wo || !x_bf16 || !expert_idx || !y || !group_ok(group) || (activation != QMOE_ACT_RELU && !int4_is_gated(activation)) ||
         (y_type != QMOE_F32 && y_type != QMOE_BF16) || d_model % 8 || d_ff % 8 || reinterpret_cast<uintptr_t>(x_bf16) % 16 ||
         reinterpret_cast<uintptr_t>(y) % 4)
         return QMOE_E_INVALID_ARG;
@@ -267,10 +273,9 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     a.out_by_slot = 1;
     a.activation = activation;
     fill_shape(&a, d_ff, d_model, group);
-    const int per_expert = (n_tokens + n_experts - 1) / n_experts;
     const int items = std::min(n_tokens, n_experts + n_tokens / kMmTokens);
-    (void)per_expert;
-    if ((st = launch_rows_kernel(a, 4, items, di.cus, s)) != QMOE_OK) return st;
+    const bool mm = n_tokens >= 4 * n_experts && n_tokens > 64;
+    if ((st = mm ? launch_mm_kernel(a, true, di.cus, s) : launch_rows_kernel(a, 4, items, di.cus, s)) != QMOE_OK) return st;
     a.mats = wo;
     a.x = g.hidden;
     a.ld_x = d_ff;
@@ -282,7 +287,7 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     a.gate = gate;
     a.activation = QMOE_ACT_NONE;
     fill_shape(&a, d_model, d_ff, group);
-    return launch_rows_kernel(a, 4, items, di.cus, s);
+    return mm ? launch_mm_kernel(a, true, di.cus, s) : launch_rows_kernel(a, 4, items, di.cus, s);
 }
 
 }  // extern "C"

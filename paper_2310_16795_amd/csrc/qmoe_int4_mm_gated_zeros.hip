@@ -1,0 +1,8 @@
+// k_int4_mm, gated, with zero points.
+#include "qmoe_int4_mm.h"
+
+namespace qmoe {
+
+qmoe_status launch_int4_mm_gated_zeros(const Int4Args &a, int cus, hipStream_t s) { return launch_mm<true, true>(a, cus, s); }
+
+}  // namespace qmoe

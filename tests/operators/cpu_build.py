@@ -7,7 +7,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, os.path.join(os.path.dirname(HERE), "lanes"))
 import cpu_build as lanes_build  # noqa: E402
 
-UNITS = ["qmoe_norm.hip", "qmoe_route.hip", "qmoe_int4.hip", "qmoe_int4_mm.hip", "qmoe_int4_host.cpp"]
+UNITS = ["qmoe_norm.hip", "qmoe_route.hip", "qmoe_int4.hip", "qmoe_int4_mm_plain.hip", "qmoe_int4_mm_zeros.hip", "qmoe_int4_mm_gated.hip",
+         "qmoe_int4_mm_gated_zeros.hip", "qmoe_int4_host.cpp"]
 MORE = r"""#pragma once
 #include <hip/hip_runtime.h>
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, ...) lanes_mfma(a, b, c)
@@ -49,9 +50,8 @@ def build(into: str) -> str:
     with open(os.path.join(src, "operators_cpu.h"), "w") as f:
         f.write(MORE)
     plain, units = lanes_build.converted, lanes_build.UNITS
-    have = [u for u in UNITS if os.path.exists(os.path.join(lanes_build.CSRC, u))]
     lanes_build.converted = lambda text: '#include "operators_cpu.h"\n' + plain(text)
-    lanes_build.UNITS = units + have
+    lanes_build.UNITS = units + UNITS
     more, lanes_build.NO_MATRIX_CORES = lanes_build.NO_MATRIX_CORES, lanes_build.NO_MATRIX_CORES + ROUND
     try:
         return lanes_build.build(into)
