@@ -629,21 +629,22 @@ qmoe_status layer_workspace_ok(int n_tokens, int n_experts, int d_model, int d_f
     return QMOE_OK;
 }
 
-qmoe_status group_by_expert(const int32_t *expert_idx, int n_tokens, int n_experts, int d_model, int d_ff, void *workspace, float *y,
-                            int row_words, hipStream_t s, GroupedTokens *out)
+qmoe_status group_by_expert(const int32_t *expert_idx, int n_tokens, int n_experts, int d_model, int d_ff, int few_tile, int many_from,
+                            void *workspace, float *y, int row_words, hipStream_t s, GroupedTokens *out)
 {
     qmoe_ws_layout l;
     const qmoe_status st = qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens, &l);
     if (st != QMOE_OK) return st;
     const LayerPtrs lp = layer_ptrs(workspace, l);
-    MmPlan all;  // every expert's tokens in tiles of kMmTokens
-    all.min_tokens = all.otherwise = 1;
-    out->items = lp.items_mm;
-    out->n_items = lp.counters + kCounterMm;
+    MmPlan mp;
+    mp.min_tokens = mp.otherwise = many_from;
+    out->few = lp.items_wi;
+    out->n_few = lp.counters + kCounterFew;
+    out->many = lp.items_mm;
+    out->n_many = lp.counters + kCounterMm;
     out->perm = lp.perm;
     out->hidden = lp.hidden;
-    out->max_items = n_tokens;
-    return launch_dispatch(dispatch_args(expert_idx, n_tokens, n_experts, row_words, lp, 4, 4, all, y), s);
+    return launch_dispatch(dispatch_args(expert_idx, n_tokens, n_experts, row_words, lp, few_tile, few_tile, mp, y), s);
 }
 }  // namespace qmoe
 

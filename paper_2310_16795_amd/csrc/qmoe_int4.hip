@@ -5,27 +5,32 @@ namespace qmoe {
 namespace {
 
 constexpr int kInt4MaxSplit = 8;
+constexpr int kInt4FewTokens = 16;  // of an expert: a tile of k_int4_rows
+constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens leave all of them to it
 
-// Sixteen rows of a matrix (gated: and the sixteen of the other projection) times up to 16 * TILES tokens.
+// Two tiles of sixteen rows of a matrix (gated: of the gate and the same ones of the other projection) times up to 16 * TILES tokens.
 //
 // v_mfma_f32_16x16x32_bf16 takes 16 tokens as its first operand and 16 rows as its second, so a result lane holds one
 // row and four tokens and needs one scale.  A lane's 16 bytes of a row are its operands for four steps of 32 columns; weights go
 // straight from memory into them, each read once per tile of tokens, and become 16 + q with two instructions a pair.
 // What the zero points (and the 16) take off is (16 + z) * sum of x over the group: a second MFMA with ones gives those
 // sums in the place where they are needed; the matrix cores have the time, since reading the weights is what bounds the kernel.
+// Two tiles of rows share what is read of x, which goes through the same path as the weights.
 // `split` wavefronts share the rows along the columns, so that a single matrix fills the GPU, and join through LDS
 // in a fixed order.
-template <int TILES, bool GATED>
-__global__ __launch_bounds__(512) void k_int4_rows(const Int4Args a)
+template <int TILES, int PER_BLOCK>
+__global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_rows(const Int4Args a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
-    constexpr int SIDES = GATED ? 2 : 1;
-    constexpr int AHEAD = TILES == 1 ? 4 : 2;  // blocks whose weights are asked for together
+    constexpr int AHEAD = TILES == 1 && PER_BLOCK < 4 ? 4 : 2;  // blocks whose weights are asked for together
+    constexpr int GROUPS = AHEAD * PER_BLOCK;                   // ... and the groups in them
     f32x4 *joined = reinterpret_cast<f32x4 *>(smem);
+    const bool gated = a.activation == QMOE_ACT_SILU_GATED || a.activation == QMOE_ACT_GELU_GATED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int part = wave % a.split, in_group = wave / a.split, side_by_side = (int)(blockDim.x >> 6) / a.split;
     const int n16 = lane & 15, quarter = lane >> 4;
-    const int row_tiles = (a.rows + 15) / 16, units_per_item = (row_tiles + side_by_side - 1) / side_by_side;
+    const int unit_rows = gated ? 16 : 32;
+    const int row_tiles = (a.rows + unit_rows - 1) / unit_rows, units_per_item = (row_tiles + side_by_side - 1) / side_by_side;
     const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + 16 * TILES - 1) / (16 * TILES);
     const long long total = (long long)n_items * units_per_item;
     const int b0 = (int)((long long)a.blocks * part / a.split), b1 = (int)((long long)a.blocks * (part + 1) / a.split);
@@ -39,11 +44,11 @@ __global__ __launch_bounds__(512) void k_int4_rows(const Int4Args a)
             expert = it.expert, slot0 = it.slot0, ntok = min(it.ntok, 16 * TILES);
         }
         const Int4Matrix m = int4_matrix(a, expert);
-        const uint8_t *w_row[SIDES];
-        size_t meta[SIDES];
+        const uint8_t *w_row[2];
+        size_t meta[2];
 #pragma unroll
-        for (int g = 0; g < SIDES; g++) {
-            const int r = min(16 * tile + n16, a.rows - 1) + g * a.rows;
+        for (int g = 0; g < 2; g++) {
+            const int r = gated ? min(16 * tile + n16, a.rows - 1) + g * a.rows : min(32 * tile + 16 * g + n16, a.rows - 1);
             w_row[g] = m.weights + (size_t)r * row_bytes + 16 * quarter;
             meta[g] = (size_t)r * a.groups;
         }
@@ -53,100 +58,115 @@ __global__ __launch_bounds__(512) void k_int4_rows(const Int4Args a)
             const int slot = slot0 + min(16 * t + n16, ntok - 1);
             x_row[t] = a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
         }
-        f32x4 acc[SIDES][TILES], sum[SIDES][TILES], ones_sum[TILES];
+        f32x4 acc[2][TILES], sum[2][TILES], ones_sum[TILES];
 #pragma unroll
         for (int t = 0; t < TILES; t++) {
             ones_sum[t] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-            for (int g = 0; g < SIDES; g++) acc[g][t] = sum[g][t] = (f32x4){0, 0, 0, 0};
+            for (int g = 0; g < 2; g++) acc[g][t] = sum[g][t] = (f32x4){0, 0, 0, 0};
         }
         for (int b = b0; b < b1; b += AHEAD) {
-            u32x4 w[AHEAD][SIDES];
-            float scale[AHEAD][SIDES][4], zero[AHEAD][SIDES][4];
+            u32x4 w[AHEAD][2];
+            uint32_t scales[2][(GROUPS + 1) / 2], zeros[2][(GROUPS + 3) / 4];  // as they stand in memory
 #pragma unroll
-            for (int u = 0; u < AHEAD; u++) {
-                const int blk = min(b + u, b1 - 1);
+            for (int u = 0; u < AHEAD; u++)
 #pragma unroll
-                for (int g = 0; g < SIDES; g++) w[u][g] = *(gp_u32x4)(w_row[g] + (size_t)64 * blk);
-            }
+                for (int g = 0; g < 2; g++) w[u][g] = *(gp_u32x4)(w_row[g] + (size_t)64 * min(b + u, b1 - 1));
+            const int g0 = PER_BLOCK * b;
+            if (a.blocks_per_group == 1 && g0 + GROUPS <= a.groups) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; u++) {
-                const int blk = min(b + u, b1 - 1);
+                for (int g = 0; g < 2; g++) {
+                    __builtin_memcpy(scales[g], m.scale + meta[g] + g0, 2 * GROUPS);
+                    if (m.zero) __builtin_memcpy(zeros[g], m.zero + meta[g] + g0, GROUPS);
+                }
+            } else {
 #pragma unroll
-                for (int g = 0; g < SIDES; g++)
+                for (int g = 0; g < 2; g++) {
 #pragma unroll
-                    for (int s = 0; s < 4; s++) {
-                        // the group that ends with step s, if one does
-                        if (((s + 1) * a.per_block) & 3) continue;
-                        const int of = a.blocks_per_group > 1 ? blk / a.blocks_per_group
-                                                              : blk * a.per_block + ((s + 1) * a.per_block) / 4 - 1;
+                    for (int i = 0; i < (GROUPS + 1) / 2; i++) scales[g][i] = 0;
+#pragma unroll
+                    for (int i = 0; i < (GROUPS + 3) / 4; i++) zeros[g][i] = 0;
+#pragma unroll
+                    for (int i = 0; i < GROUPS; i++) {
+                        const int of = a.blocks_per_group > 1 ? min(b + i, b1 - 1) / a.blocks_per_group : g0 + i;
                         const size_t at = meta[g] + min(of, a.groups - 1);
-                        scale[u][g][s] = half_bits_to_float(m.scale[at]);
-                        zero[u][g][s] = m.zero ? 16.0f + (float)m.zero[at] : 24.0f;
+                        scales[g][i / 2] |= (uint32_t)m.scale[at] << (16 * (i % 2));
+                        if (m.zero) zeros[g][i / 4] |= (uint32_t)m.zero[at] << (8 * (i % 4));
                     }
+                }
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; u++) {
                 if (b + u >= b1) break;
                 const int c = kInt4BlockCols * (b + u) + 8 * quarter;
+                u32x4 x[TILES][4];
+#pragma unroll
+                for (int t = 0; t < TILES; t++)
+#pragma unroll
+                    for (int s = 0; s < 4; s++) x[t][s] = int4_x(x_row[t], c + 32 * s, a.cols);
 #pragma unroll
                 for (int s = 0; s < 4; s++) {
-                    bf16x8 wf[SIDES];
-#pragma unroll
-                    for (int g = 0; g < SIDES; g++) wf[g] = int4_plus16(w[u][g][s]);
+                    const bf16x8 w0 = int4_plus16(w[u][0][s]), w1 = int4_plus16(w[u][1][s]);
 #pragma unroll
                     for (int t = 0; t < TILES; t++) {
-                        const bf16x8 xf = __builtin_bit_cast(bf16x8, int4_x(x_row[t], c + 32 * s, a.cols));
+                        const bf16x8 xf = __builtin_bit_cast(bf16x8, x[t][s]);
                         ones_sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, ones, ones_sum[t], 0, 0, 0);
-#pragma unroll
-                        for (int g = 0; g < SIDES; g++)
-                            sum[g][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, wf[g], sum[g][t], 0, 0, 0);
+                        sum[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w0, sum[0][t], 0, 0, 0);
+                        sum[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w1, sum[1][t], 0, 0, 0);
                     }
-                    if (((s + 1) * a.per_block) & 3) continue;
+                    if ((s + 1) * PER_BLOCK % 4) continue;
+                    const int i = u * PER_BLOCK + (s + 1) * PER_BLOCK / 4 - 1;
 #pragma unroll
-                    for (int t = 0; t < TILES; t++) {
+                    for (int g = 0; g < 2; g++) {
+                        const float scale = half_bits_to_float((uint16_t)(scales[g][i / 2] >> (16 * (i % 2))));
+                        const float zero = m.zero ? 16.0f + (float)((zeros[g][i / 4] >> (8 * (i % 4))) & 255u) : 24.0f;
 #pragma unroll
-                        for (int g = 0; g < SIDES; g++) {
+                        for (int t = 0; t < TILES; t++) {
 #pragma unroll
-                            for (int i = 0; i < 4; i++)
-                                acc[g][t][i] = fmaf(scale[u][g][s], fmaf(-zero[u][g][s], ones_sum[t][i], sum[g][t][i]), acc[g][t][i]);
+                            for (int k = 0; k < 4; k++)
+                                acc[g][t][k] = fmaf(scale, fmaf(-zero, ones_sum[t][k], sum[g][t][k]), acc[g][t][k]);
                             sum[g][t] = (f32x4){0, 0, 0, 0};
                         }
-                        ones_sum[t] = (f32x4){0, 0, 0, 0};
                     }
+#pragma unroll
+                    for (int t = 0; t < TILES; t++) ones_sum[t] = (f32x4){0, 0, 0, 0};
                 }
             }
         }
+        f32x4 *mine = joined + (size_t)(in_group * a.split) * 2 * TILES * 64;
         if (a.split > 1) {
-            f32x4 *mine = joined + (size_t)(in_group * a.split) * SIDES * TILES * 64;
 #pragma unroll
-            for (int g = 0; g < SIDES; g++)
+            for (int g = 0; g < 2; g++)
 #pragma unroll
-                for (int t = 0; t < TILES; t++) mine[((part * SIDES + g) * TILES + t) * 64 + lane] = acc[g][t];
+                for (int t = 0; t < TILES; t++) mine[((part * 2 + g) * TILES + t) * 64 + lane] = acc[g][t];
             __syncthreads();
         }
-        const int r = 16 * tile + n16;
 #pragma unroll
         for (int t = 0; t < TILES; t++) {
             if (t % a.split != part) continue;  // a tile of tokens is joined by one of the wavefronts
             if (16 * t >= ntok) break;
             if (a.split > 1) {
-                const f32x4 *mine = joined + (size_t)(in_group * a.split) * SIDES * TILES * 64;
 #pragma unroll
-                for (int g = 0; g < SIDES; g++) {
+                for (int g = 0; g < 2; g++) {
                     f32x4 v = mine[(g * TILES + t) * 64 + lane];
-                    for (int p = 1; p < a.split; p++) v += mine[((p * SIDES + g) * TILES + t) * 64 + lane];
+                    for (int p = 1; p < a.split; p++) v += mine[((p * 2 + g) * TILES + t) * 64 + lane];
                     acc[g][t] = v;
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int in_tile = 16 * t + 4 * quarter + i;
-                if (in_tile >= ntok || r >= a.rows) continue;
+            for (int k = 0; k < 4; k++) {
+                const int in_tile = 16 * t + 4 * quarter + k;
+                if (in_tile >= ntok) continue;
                 const int token = a.perm ? a.perm[slot0 + in_tile] : slot0 + in_tile;
-                float v = acc[0][t][i];
-                if constexpr (GATED) v = int4_gated(v, acc[1][t][i], a.activation);
-                int4_store(a, a.out_by_slot ? slot0 + in_tile : token, a.gate ? a.gate[token] : 1.0f, r, v);
+                const size_t out_row = a.out_by_slot ? slot0 + in_tile : token;
+                const float gate = a.gate ? a.gate[token] : 1.0f;
+                const int r = unit_rows * tile + n16;
+                if (gated) {
+                    if (r < a.rows) int4_store(a, out_row, gate, r, int4_gated(acc[0][t][k], acc[1][t][k], a.activation));
+                } else {
+                    if (r < a.rows) int4_store(a, out_row, gate, r, acc[0][t][k]);
+                    if (r + 16 < a.rows) int4_store(a, out_row, gate, r + 16, acc[1][t][k]);
+                }
             }
         }
         if (a.split > 1) __syncthreads();  // before the next unit's sums overwrite these
@@ -166,19 +186,13 @@ void fill_shape(Int4Args *a, int rows, int cols, int group)
     a->blocks_per_group = group < kInt4BlockCols ? 1 : group / kInt4BlockCols;
 }
 
-template <int TILES>
-qmoe_status launch_tiles(const Int4Args &a, int grid, int threads, hipStream_t s)
+template <int TILES, int PER_BLOCK>
+qmoe_status launch_rows_variant(const Int4Args &a, int grid, int threads, hipStream_t s)
 {
-    const size_t smem = a.split > 1 ? (size_t)(threads / 64) * (int4_is_gated(a.activation) ? 2 : 1) * TILES * 64 * sizeof(f32x4) : 0;
-    if (int4_is_gated(a.activation)) {
-        const qmoe_status st = allow_lds(k_int4_rows<TILES, true>, smem);
-        if (st != QMOE_OK) return st;
-        hipLaunchKernelGGL((k_int4_rows<TILES, true>), dim3(grid), dim3(threads), smem, s, a);
-    } else {
-        const qmoe_status st = allow_lds(k_int4_rows<TILES, false>, smem);
-        if (st != QMOE_OK) return st;
-        hipLaunchKernelGGL((k_int4_rows<TILES, false>), dim3(grid), dim3(threads), smem, s, a);
-    }
+    const size_t smem = a.split > 1 ? (size_t)(threads / 64) * 2 * TILES * 64 * sizeof(f32x4) : 0;
+    const qmoe_status st = allow_lds(k_int4_rows<TILES, PER_BLOCK>, smem);
+    if (st != QMOE_OK) return st;
+    hipLaunchKernelGGL((k_int4_rows<TILES, PER_BLOCK>), dim3(grid), dim3(threads), smem, s, a);
     QMOE_HIP_TRY(hipGetLastError());
     return QMOE_OK;
 }
@@ -186,16 +200,26 @@ qmoe_status launch_tiles(const Int4Args &a, int grid, int threads, hipStream_t s
 // tiles: tiles of 16 tokens of an item; items: how many the call has, about
 qmoe_status launch_rows_kernel(Int4Args a, int tiles, long long items, int cus, hipStream_t s)
 {
-    const long long units = items * ((a.rows + 15) / 16);
+    const int unit_rows = int4_is_gated(a.activation) ? 16 : 32, row_tiles = (a.rows + unit_rows - 1) / unit_rows;
+    const long long units = items * row_tiles;
     a.split = 1;
     while (a.split < kInt4MaxSplit && units * a.split < 8LL * cus && 2 * a.split <= a.blocks) a.split *= 2;
     const int threads = 64 * (a.split < 4 ? 4 : a.split);
     const int side_by_side = threads / 64 / a.split;
-    const long long groups = items * (((a.rows + 15) / 16 + side_by_side - 1) / side_by_side);
+    const long long groups = items * ((row_tiles + side_by_side - 1) / side_by_side);
     const int grid = (int)std::min<long long>(groups, 64LL * cus);
-    if (tiles <= 1) return launch_tiles<1>(a, grid, threads, s);
-    if (tiles <= 2) return launch_tiles<2>(a, grid, threads, s);
-    return launch_tiles<4>(a, grid, threads, s);
+    const int variant = (tiles <= 1 ? 0 : tiles <= 2 ? 3 : 6) + (a.per_block == 1 ? 0 : a.per_block == 2 ? 1 : 2);
+    switch (variant) {
+    case 0: return launch_rows_variant<1, 1>(a, grid, threads, s);
+    case 1: return launch_rows_variant<1, 2>(a, grid, threads, s);
+    case 2: return launch_rows_variant<1, 4>(a, grid, threads, s);
+    case 3: return launch_rows_variant<2, 1>(a, grid, threads, s);
+    case 4: return launch_rows_variant<2, 2>(a, grid, threads, s);
+    case 5: return launch_rows_variant<2, 4>(a, grid, threads, s);
+    case 6: return launch_rows_variant<4, 1>(a, grid, threads, s);
+    case 7: return launch_rows_variant<4, 2>(a, grid, threads, s);
+    default: return launch_rows_variant<4, 4>(a, grid, threads, s);
+    }
 }
 
 // zeros: a matrix has zero points (descriptors in device memory: may have)
@@ -255,15 +279,14 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     hipStream_t s = static_cast<hipStream_t>(stream);
     DeviceInfo di;
     if ((st = gpu_info(&di)) != QMOE_OK) return st;
+    const bool crowded = n_tokens > kInt4AllFew;
     GroupedTokens g;
-    if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, workspace, static_cast<float *>(y),
+    if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, kInt4FewTokens,
+                              crowded ? kInt4FewTokens + 1 : 0x7FFFFFFF, workspace, static_cast<float *>(y),
                               y_type == QMOE_F32 ? d_model : d_model / 2, s, &g)) != QMOE_OK)
         return st;
     Int4Args a{};
     a.mats = wi;
-    a.items = g.items;
-    a.n_items_dev = g.n_items;
-    a.max_items = g.max_items;
     a.n_experts = n_experts;
     a.perm = g.perm;
     a.x = x_bf16;
@@ -273,9 +296,18 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     a.out_by_slot = 1;
     a.activation = activation;
     fill_shape(&a, d_ff, d_model, group);
-    const int items = std::min(n_tokens, n_experts + n_tokens / kMmTokens);
-    const bool mm = n_tokens >= 4 * n_experts && n_tokens > 64;
-    if ((st = mm ? launch_mm_kernel(a, true, di.cus, s) : launch_rows_kernel(a, 4, items, di.cus, s)) != QMOE_OK) return st;
+    auto product = [&]() {
+        a.items = g.few;
+        a.n_items_dev = g.n_few;
+        a.max_items = std::min(n_tokens, n_experts + n_tokens / kInt4FewTokens);
+        qmoe_status r = launch_rows_kernel(a, 1, a.max_items, di.cus, s);
+        if (r != QMOE_OK || !crowded) return r;
+        a.items = g.many;
+        a.n_items_dev = g.n_many;
+        a.max_items = n_tokens / kInt4FewTokens;  // (each has more than that, or stands beside a whole tile)
+        return launch_mm_kernel(a, true, di.cus, s);
+    };
+    if ((st = product()) != QMOE_OK) return st;
     a.mats = wo;
     a.x = g.hidden;
     a.ld_x = d_ff;
@@ -287,7 +319,7 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     a.gate = gate;
     a.activation = QMOE_ACT_NONE;
     fill_shape(&a, d_model, d_ff, group);
-    return mm ? launch_mm_kernel(a, true, di.cus, s) : launch_rows_kernel(a, 4, items, di.cus, s);
+    return product();
 }
 
 }  // extern "C"
