@@ -26,7 +26,8 @@ struct Int4Args {
     int cols, blocks, groups;
     int per_block, blocks_per_group;  // groups a block (1, 2, 4), blocks a group (1 or more)
     int activation;
-    int split;                     // k_int4_rows: wavefronts that share a tile of rows along the columns
+    int split, reps;               // k_int4_rows: wavefronts that share a tile of rows along the columns, tiles of a wavefront
+    uint32_t x_bytes;              // ... and LDS for activations
 };
 
 // One matrix as a wavefront reads it.
