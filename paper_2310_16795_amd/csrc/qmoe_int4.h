@@ -27,7 +27,7 @@ struct Int4Args {
     int per_block, blocks_per_group;  // groups a block (1, 2, 4), blocks a group (1 or more)
     int activation;
     int split, reps;               // k_int4_rows: wavefronts that share a tile of rows along the columns, tiles of a wavefront
-    uint32_t x_bytes;              // ... and LDS for activations
+    uint32_t x_bytes, sum_bytes;   // ... LDS for activations, for their sums by group
 };
 
 // One matrix as a wavefront reads it.
@@ -44,10 +44,13 @@ __device__ __forceinline__ Int4Matrix int4_matrix(const Int4Args &a, int expert)
 }
 
 // Eight weights (a word) as bf16 16 + q, in the order of their columns: bits 3..6 of a bf16 between 16 and 32 are its
-// units, so a shift and a mask do for two, exactly.  The 16 goes with the zero point, against the sum of x.
+// units, so a shift and an and-or do for two, exactly.  The 16 goes with the zero point, against the sum of x.
+// The two constants are hidden from the compiler, which knows no and-or with literals (and takes three instructions).
 __device__ __forceinline__ bf16x8 int4_plus16(uint32_t w)
 {
-    const uint32_t m = 0x00780078u, b = 0x41804180u;
+    uint32_t m = 0x00780078u, b = 0x41804180u;
+    asm("" : "+s"(m));
+    asm("" : "+v"(b));
     const u32x4 v = {((w << 3) & m) | b, ((w >> 1) & m) | b, ((w >> 5) & m) | b, ((w >> 9) & m) | b};
     return __builtin_bit_cast(bf16x8, v);
 }
@@ -61,6 +64,21 @@ __device__ __forceinline__ u32x4 int4_x(const uint16_t *row, int c, int cols)
     for (int i = 0; i < 8; i++)
         if (c + i < cols) v[i / 2] |= (uint32_t)row[c + i] << (16 * (i % 2));
     return v;
+}
+
+// The sum of x over a group, in the last of the lanes (of 16 that hold the 128 columns of a token's block) whose columns the group is.
+template <int PER_BLOCK>
+__device__ __forceinline__ float int4_group_sum(u32x4 x)
+{
+    const bf16x2 one = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; i++) s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)x[i]), one, s, false);
+    s += dpp_f<0x111, 0xf>(0.0f, s);
+    s += dpp_f<0x112, 0xf>(0.0f, s);
+    if constexpr (PER_BLOCK <= 2) s += dpp_f<0x114, 0xf>(0.0f, s);
+    if constexpr (PER_BLOCK == 1) s += dpp_f<0x118, 0xf>(0.0f, s);
+    return s;
 }
 
 inline bool int4_is_gated(int activation) { return activation == QMOE_ACT_SILU_GATED || activation == QMOE_ACT_GELU_GATED; }

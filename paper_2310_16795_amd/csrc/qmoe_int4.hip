@@ -5,7 +5,7 @@ namespace qmoe {
 namespace {
 
 constexpr int kInt4MaxSplit = 8;
-constexpr size_t kInt4XBytes = 48 * 1024;  // of activations in a workgroup's LDS: 64 tokens' 256 columns and more
+constexpr size_t kInt4XBytes = 32 * 1024;  // of activations in a workgroup's LDS: 64 tokens' 256 columns and more
 constexpr int kInt4FewTokens = 16;  // of an expert: a tile of k_int4_rows
 constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens leave all of them to it
 
@@ -13,9 +13,8 @@ constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens leave
 //
 // v_mfma_f32_16x16x32_bf16 takes 16 tokens as its first operand and 16 rows as its second, so a result lane holds one
 // row and four tokens and needs one scale.  16 bytes of a row are a lane's operands for four steps of 32 columns and become 16 + q with two
-// instructions a pair.  What the zero points (and the 16) take off is (16 + z) * sum of x over the group: a second MFMA with ones
-// gives those sums in the place where they are needed; the matrix cores have the time, since reading the weights is what bounds
-// the kernel.
+// instructions a pair.  What the zero points (and the 16) take off is (16 + z) * sum of x over the group, where a group's sum starts;
+// the sums of x are formed by those who bring x into LDS.
 // Four neighbouring lanes load the 64 bytes that a row has in a block (one access of the cache; a load in the operands' order, a row a
 // lane, is four), and ds_bpermute brings them to their lanes.  Scales come for four steps at a time, a step's to a quarter of the
 // wavefront each.  The activations of the tokens lie in LDS, a piece of the columns at a time if they must, for all wavefronts
@@ -23,13 +22,14 @@ constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens leave
 // `split` wavefronts share the rows along the columns, so that a single matrix fills the GPU, and join through LDS
 // in a fixed order.
 template <int TILES, int PER_BLOCK>
-__global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_rows(const Int4Args a)
+__global__ __launch_bounds__(64 * kInt4MaxSplit, TILES == 1 ? 4 : 2) void k_int4_rows(const Int4Args a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr int AHEAD = 2, GROUPS = AHEAD * PER_BLOCK;  // blocks of a step, and the groups in them
     constexpr int WORDS = (GROUPS + 1) / 2, ZERO_WORDS = (GROUPS + 3) / 4;
     uint16_t *s_x = reinterpret_cast<uint16_t *>(smem);
-    f32x4 *joined = reinterpret_cast<f32x4 *>(smem + a.x_bytes);
+    float *s_sum = reinterpret_cast<float *>(smem + a.x_bytes);  // [group of the piece of columns][16 * TILES tokens]
+    f32x4 *joined = reinterpret_cast<f32x4 *>(smem + a.x_bytes + a.sum_bytes);
     const bool gated = a.activation == QMOE_ACT_SILU_GATED || a.activation == QMOE_ACT_GELU_GATED;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int part = wave % a.split, in_group = wave / a.split, side_by_side = (int)(blockDim.x >> 6) / a.split;
@@ -41,7 +41,6 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_rows(const Int4Args
     const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + 16 * TILES - 1) / (16 * TILES);
     const long long total = (long long)n_items * units_per_item;
     const size_t row_bytes = (size_t)64 * a.blocks;
-    const bf16x8 ones = __builtin_bit_cast(bf16x8, (u32x4){0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
     for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
         const int item = (int)(unit / units_per_item), first_tile = (int)(unit - (long long)item * units_per_item) * unit_tiles;
         int expert = 0, slot0 = item * 16 * TILES, ntok = min(16 * TILES, a.batch - slot0);
@@ -50,7 +49,8 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_rows(const Int4Args
             expert = it.expert, slot0 = it.slot0, ntok = min(it.ntok, 16 * TILES);
         }
         const Int4Matrix m = int4_matrix(a, expert);
-        const int fit = (int)((a.x_bytes / 2 / (uint32_t)ntok - 8) / kInt4BlockCols), chunk = min(a.blocks, fit), ld_s = chunk * kInt4BlockCols + 8;
+        const int fit = (int)min((a.x_bytes / 2 / (uint32_t)ntok - 8) / kInt4BlockCols, a.sum_bytes / (4 * 16 * TILES * PER_BLOCK));
+        const int chunk = min(a.blocks, fit), ld_s = chunk * kInt4BlockCols + 8;
         for (int rep = 0; rep < a.reps; rep++) {
             if (first_tile + rep * side_by_side >= row_tiles) break;  // (for the whole workgroup)
             const int tile = first_tile + rep * side_by_side + in_group;
@@ -62,13 +62,11 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_rows(const Int4Args
                 w_row[g] = m.weights + (size_t)(min(base + (lane >> 2), a.rows - 1) + behind) * row_bytes + 16 * (lane & 3);
                 meta[g] = (size_t)(min(base + n16, a.rows - 1) + behind) * a.groups;
             }
-            f32x4 acc[2][TILES], sum[2][TILES], ones_sum[TILES];
+            f32x4 acc[2][TILES], sum[2][TILES];
 #pragma unroll
-            for (int t = 0; t < TILES; t++) {
-                ones_sum[t] = (f32x4){0, 0, 0, 0};
+            for (int t = 0; t < TILES; t++)
 #pragma unroll
-                for (int g = 0; g < 2; g++) acc[g][t] = sum[g][t] = (f32x4){0, 0, 0, 0};
-            }
+                for (int g = 0; g < 2; g++) acc[g][t] = (f32x4){0, 0, 0, 0};
             for (int c0 = 0; c0 < a.blocks; c0 += chunk) {
                 const int n_blocks = min(chunk, a.blocks - c0);
                 const int b0 = c0 + n_blocks * part / a.split, b1 = c0 + n_blocks * (part + 1) / a.split;
@@ -86,7 +84,10 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_rows(const Int4Args
                     for (int i = threadIdx.x; i < ntok * pieces; i += blockDim.x) {
                         const int token = i / pieces, c = 8 * (i - token * pieces), slot = slot0 + token;
                         const uint16_t *x = a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
-                        *reinterpret_cast<u32x4 *>(&s_x[token * ld_s + c]) = int4_x(x, kInt4BlockCols * c0 + c, a.cols);
+                        const u32x4 v = int4_x(x, kInt4BlockCols * c0 + c, a.cols);
+                        *reinterpret_cast<u32x4 *>(&s_x[token * ld_s + c]) = v;
+                        const float all = int4_group_sum<PER_BLOCK>(v);  // (16 lanes hold a block of a token)
+                        if ((lane + 1) % (16 / PER_BLOCK) == 0) s_sum[(c / (kInt4BlockCols / PER_BLOCK)) * (16 * TILES) + token] = all;
                     }
                     __syncthreads();
                 }
@@ -140,32 +141,35 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_rows(const Int4Args
                     for (int u = 0; u < AHEAD; u++) {
                         if (b + u >= b1) break;
                         const uint16_t *x_at = s_x + kInt4BlockCols * (b + u - c0) + 8 * quarter;
+                        const float *sum_at = s_sum + PER_BLOCK * (b + u - c0) * (16 * TILES) + 4 * quarter;
 #pragma unroll
                         for (int s = 0; s < 4; s++) {
+                            const int in_block = s * PER_BLOCK / 4, i = u * PER_BLOCK + in_block;
+                            if (s * PER_BLOCK % 4 == 0) {
+#pragma unroll
+                                for (int g = 0; g < 2; g++) {
+                                    const float zero = m.zero ? -16.0f - (float)((zero_of[g][i / 4] >> (8 * (i % 4))) & 255u) : -24.0f;
+#pragma unroll
+                                    for (int t = 0; t < TILES; t++)
+                                        sum[g][t] = zero * *reinterpret_cast<const f32x4 *>(sum_at + in_block * 16 * TILES + 16 * t);
+                                }
+                            }
                             const bf16x8 w0 = int4_plus16(w[u][0][s]), w1 = int4_plus16(w[u][1][s]);
 #pragma unroll
                             for (int t = 0; t < TILES; t++) {
                                 const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(x_at + min(16 * t + n16, ntok - 1) * ld_s + 32 * s);
-                                ones_sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, ones, ones_sum[t], 0, 0, 0);
                                 sum[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w0, sum[0][t], 0, 0, 0);
                                 sum[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w1, sum[1][t], 0, 0, 0);
                             }
                             if ((s + 1) * PER_BLOCK % 4) continue;
-                            const int i = u * PER_BLOCK + (s + 1) * PER_BLOCK / 4 - 1;
 #pragma unroll
                             for (int g = 0; g < 2; g++) {
                                 const float scale = half_bits_to_float((uint16_t)(scale_of[g][i / 2] >> (16 * (i % 2))));
-                                const float zero = m.zero ? 16.0f + (float)((zero_of[g][i / 4] >> (8 * (i % 4))) & 255u) : 24.0f;
 #pragma unroll
-                                for (int t = 0; t < TILES; t++) {
+                                for (int t = 0; t < TILES; t++)
 #pragma unroll
-                                    for (int k = 0; k < 4; k++)
-                                        acc[g][t][k] = fmaf(scale, fmaf(-zero, ones_sum[t][k], sum[g][t][k]), acc[g][t][k]);
-                                    sum[g][t] = (f32x4){0, 0, 0, 0};
-                                }
+                                    for (int k = 0; k < 4; k++) acc[g][t][k] = fmaf(scale, sum[g][t][k], acc[g][t][k]);
                             }
-#pragma unroll
-                            for (int t = 0; t < TILES; t++) ones_sum[t] = (f32x4){0, 0, 0, 0};
                         }
                     }
                 }
@@ -227,7 +231,7 @@ void fill_shape(Int4Args *a, int rows, int cols, int group)
 template <int TILES, int PER_BLOCK>
 qmoe_status launch_rows_variant(const Int4Args &a, int grid, int threads, hipStream_t s)
 {
-    const size_t smem = a.x_bytes + (a.split > 1 ? (size_t)(threads / 64) * 2 * TILES * 64 * sizeof(f32x4) : 0);
+    const size_t smem = a.x_bytes + a.sum_bytes + (a.split > 1 ? (size_t)(threads / 64) * 2 * TILES * 64 * sizeof(f32x4) : 0);
     const qmoe_status st = allow_lds(k_int4_rows<TILES, PER_BLOCK>, smem);
     if (st != QMOE_OK) return st;
     hipLaunchKernelGGL((k_int4_rows<TILES, PER_BLOCK>), dim3(grid), dim3(threads), smem, s, a);
@@ -245,11 +249,12 @@ qmoe_status launch_rows_kernel(Int4Args a, int tiles, long long items, int cus, 
     const int threads = 64 * (a.split < 4 ? 4 : a.split);
     const int side_by_side = threads / 64 / a.split;
     // several tiles a wavefront where that leaves enough workgroups: the activations are staged once for them
-    a.reps = (int)std::min<long long>(4, std::max<long long>(1, items * row_tiles / (16LL * cus * side_by_side)));
+    a.reps = (int)std::min<long long>(2, std::max<long long>(1, items * row_tiles / (16LL * cus * side_by_side)));
     const long long groups = items * ((row_tiles + side_by_side * a.reps - 1) / (side_by_side * a.reps));
     const int tokens = 16 * (tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4);
     a.x_bytes = (uint32_t)std::min<size_t>(kInt4XBytes, (size_t)tokens * 2 * (a.blocks * kInt4BlockCols + 8));
     const int grid = (int)std::min<long long>(groups, 64LL * cus);
+    a.sum_bytes = (uint32_t)std::min<size_t>(kInt4XBytes / 4, (size_t)tokens * 4 * a.blocks * a.per_block);
     const int variant = (tiles <= 1 ? 0 : tiles <= 2 ? 3 : 6) + (a.per_block == 1 ? 0 : a.per_block == 2 ? 1 : 2);
     switch (variant) {
     case 0: return launch_rows_variant<1, 1>(a, grid, threads, s);

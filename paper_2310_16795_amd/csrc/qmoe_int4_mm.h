@@ -79,14 +79,7 @@ __global__ __launch_bounds__(64 * kMmWaves, TILES == 8 ? 1 : 2) void k_int4_mm(c
                 if (t >= tiles) break;
                 const int token = 16 * t + stager;
                 *reinterpret_cast<u32x4 *>(&s_x[buf][token * kXRow + 8 * piece]) = x_next[t];
-                const bf16x2 one = __builtin_bit_cast(bf16x2, 0x3F803F80u);
-                float s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; i++) s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)x_next[t][i]), one, s, false);
-                s += dpp_f<0x111, 0xf>(0.0f, s);
-                s += dpp_f<0x112, 0xf>(0.0f, s);
-                if constexpr (PER_BLOCK <= 2) s += dpp_f<0x114, 0xf>(0.0f, s);
-                if constexpr (PER_BLOCK == 1) s += dpp_f<0x118, 0xf>(0.0f, s);
+                const float s = int4_group_sum<PER_BLOCK>(x_next[t]);
                 if ((piece + 1) % (16 / PER_BLOCK) == 0) s_sum[buf][piece / (16 / PER_BLOCK)][token] = ZEROS ? s : -24.0f * s;
             }
         };
