@@ -26,8 +26,7 @@ struct Int4Args {
     int cols, blocks, groups;
     int per_block, blocks_per_group;  // groups a block (1, 2, 4), blocks a group (1 or more)
     int activation;
-    int split, reps;               // k_int4_rows: wavefronts that share a tile of rows along the columns, tiles of a wavefront
-    uint32_t x_bytes, sum_bytes;   // ... LDS for activations, for their sums by group
+    int split;                     // k_int4_split: wavefronts that share a tile of rows along the columns
 };
 
 // One matrix as a wavefront reads it.

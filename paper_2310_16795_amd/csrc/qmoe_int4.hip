@@ -5,212 +5,339 @@ namespace qmoe {
 namespace {
 
 constexpr int kInt4MaxSplit = 8;
-constexpr size_t kInt4XBytes = 32 * 1024;  // of activations in a workgroup's LDS: 64 tokens' 256 columns and more
-constexpr int kInt4FewTokens = 16;  // of an expert: a tile of k_int4_rows
-constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens leave all of them to it
+constexpr int kInt4FewTokens = 16;  // of an expert: one tile of tokens; those with more get four
+constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens make no tiles but of 16
 
-// Two tiles of sixteen rows of a matrix (gated: of the gate and the same ones of the other projection) times up to 16 * TILES tokens.
+// What both kernels here share.
 //
 // v_mfma_f32_16x16x32_bf16 takes 16 tokens as its first operand and 16 rows as its second, so a result lane holds one
 // row and four tokens and needs one scale.  16 bytes of a row are a lane's operands for four steps of 32 columns and become 16 + q with two
 // instructions a pair.  What the zero points (and the 16) take off is (16 + z) * sum of x over the group, where a group's sum starts;
 // the sums of x are formed by those who bring x into LDS.
 // Four neighbouring lanes load the 64 bytes that a row has in a block (one access of the cache; a load in the operands' order, a row a
-// lane, is four), and ds_bpermute brings them to their lanes.  Scales come for four steps at a time, a step's to a quarter of the
-// wavefront each.  The activations of the tokens lie in LDS, a piece of the columns at a time if they must, for all wavefronts
-// of the workgroup and `reps` tiles of each.
-// `split` wavefronts share the rows along the columns, so that a single matrix fills the GPU, and join through LDS
-// in a fixed order.
-template <int TILES, int PER_BLOCK>
-__global__ __launch_bounds__(64 * kInt4MaxSplit, TILES == 1 ? 4 : 2) void k_int4_rows(const Int4Args a)
-{
-    extern __shared__ __align__(16) unsigned char smem[];
-    constexpr int AHEAD = 2, GROUPS = AHEAD * PER_BLOCK;  // blocks of a step, and the groups in them
-    constexpr int WORDS = (GROUPS + 1) / 2, ZERO_WORDS = (GROUPS + 3) / 4;
-    uint16_t *s_x = reinterpret_cast<uint16_t *>(smem);
-    float *s_sum = reinterpret_cast<float *>(smem + a.x_bytes);  // [group of the piece of columns][16 * TILES tokens]
-    f32x4 *joined = reinterpret_cast<f32x4 *>(smem + a.x_bytes + a.sum_bytes);
-    const bool gated = a.activation == QMOE_ACT_SILU_GATED || a.activation == QMOE_ACT_GELU_GATED;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int part = wave % a.split, in_group = wave / a.split, side_by_side = (int)(blockDim.x >> 6) / a.split;
-    const int n16 = lane & 15, quarter = lane >> 4;
-    const int from_lane = 4 * (4 * n16 + quarter);  // whose load holds this lane's operands, in bytes
-    const int unit_rows = gated ? 16 : 32;
-    const int row_tiles = (a.rows + unit_rows - 1) / unit_rows, unit_tiles = side_by_side * a.reps;
-    const int units_per_item = (row_tiles + unit_tiles - 1) / unit_tiles;
-    const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + 16 * TILES - 1) / (16 * TILES);
-    const long long total = (long long)n_items * units_per_item;
-    const size_t row_bytes = (size_t)64 * a.blocks;
-    for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
-        const int item = (int)(unit / units_per_item), first_tile = (int)(unit - (long long)item * units_per_item) * unit_tiles;
-        int expert = 0, slot0 = item * 16 * TILES, ntok = min(16 * TILES, a.batch - slot0);
-        if (a.items) {
-            const Item it = a.items[item];
-            expert = it.expert, slot0 = it.slot0, ntok = min(it.ntok, 16 * TILES);
-        }
-        const Int4Matrix m = int4_matrix(a, expert);
-        const int fit = (int)min((a.x_bytes / 2 / (uint32_t)ntok - 8) / kInt4BlockCols, a.sum_bytes / (4 * 16 * TILES * PER_BLOCK));
-        const int chunk = min(a.blocks, fit), ld_s = chunk * kInt4BlockCols + 8;
-        for (int rep = 0; rep < a.reps; rep++) {
-            if (first_tile + rep * side_by_side >= row_tiles) break;  // (for the whole workgroup)
-            const int tile = first_tile + rep * side_by_side + in_group;
-            const uint8_t *w_row[2];
-            size_t meta[2];
+// lane, is four), and ds_bpermute brings them to their lanes.  A lane's scales come for BLOCKS blocks at a time, those of the next 4 * BLOCKS in one
+// load, a quarter of the wavefront each.
+
+// SIDES tiles of 16 rows: their weights and scales, as a lane loads them.
+template <int SIDES, int BLOCKS, int PER_BLOCK>
+struct Int4Rows {
+    static constexpr int GROUPS = BLOCKS * PER_BLOCK, WORDS = (GROUPS + 1) / 2, ZERO_WORDS = (GROUPS + 3) / 4;
+    const uint8_t *row[SIDES];
+    size_t meta[SIDES];
+    u32x4 next[BLOCKS][SIDES];
+    uint32_t scales[SIDES][WORDS], zeros[SIDES][ZERO_WORDS];
+
+    // the tile's first row on each side, and what stands behind it in the matrix (the other projection)
+    __device__ __forceinline__ void at(const Int4Args &a, const Int4Matrix &m, int lane, const int (&base)[SIDES], const int (&behind)[SIDES])
+    {
+        const size_t row_bytes = (size_t)64 * a.blocks;
 #pragma unroll
-            for (int g = 0; g < 2; g++) {
-                const int base = gated ? 16 * tile : 32 * tile + 16 * g, behind = gated ? g * a.rows : 0;
-                w_row[g] = m.weights + (size_t)(min(base + (lane >> 2), a.rows - 1) + behind) * row_bytes + 16 * (lane & 3);
-                meta[g] = (size_t)(min(base + n16, a.rows - 1) + behind) * a.groups;
+        for (int g = 0; g < SIDES; g++) {
+            row[g] = m.weights + (size_t)(min(base[g] + (lane >> 2), a.rows - 1) + behind[g]) * row_bytes + 16 * (lane & 3);
+            meta[g] = (size_t)(min(base[g] + (lane & 15), a.rows - 1) + behind[g]) * a.groups;
+        }
+    }
+    __device__ __forceinline__ void load(int b, int last)
+    {
+#pragma unroll
+        for (int u = 0; u < BLOCKS; u++)
+#pragma unroll
+            for (int g = 0; g < SIDES; g++) next[u][g] = *(gp_u32x4)(row[g] + (size_t)64 * min(b + u, last));
+    }
+    // scales of the 4 * BLOCKS blocks from b on
+    __device__ __forceinline__ void load_scales(const Int4Args &a, const Int4Matrix &m, int quarter, int b)
+    {
+        const int mine = b + BLOCKS * quarter, g0 = PER_BLOCK * mine;
+        if (a.blocks_per_group == 1 && g0 + GROUPS <= a.groups) {
+#pragma unroll
+            for (int g = 0; g < SIDES; g++) {
+                __builtin_memcpy(scales[g], m.scale + meta[g] + g0, 2 * GROUPS);
+                if (m.zero) __builtin_memcpy(zeros[g], m.zero + meta[g] + g0, GROUPS);
             }
-            f32x4 acc[2][TILES], sum[2][TILES];
+            return;
+        }
+#pragma unroll
+        for (int g = 0; g < SIDES; g++) {
+#pragma unroll
+            for (int i = 0; i < WORDS; i++) scales[g][i] = 0;
+#pragma unroll
+            for (int i = 0; i < ZERO_WORDS; i++) zeros[g][i] = 0;
+#pragma unroll
+            for (int i = 0; i < GROUPS; i++) {
+                const int of = a.blocks_per_group > 1 ? (mine + i) / a.blocks_per_group : g0 + i;
+                const size_t at = meta[g] + min(of, a.groups - 1);
+                scales[g][i / 2] |= (uint32_t)m.scale[at] << (16 * (i % 2));
+                if (m.zero) zeros[g][i / 4] |= (uint32_t)m.zero[at] << (8 * (i % 4));
+            }
+        }
+    }
+};
+
+// A block's 128 columns: acc += scale * (sum over the group of (16 + q) x - (16 + z) * sum of x), tokens and rows of this wavefront.
+// x: this lane's first operand in LDS, a token's row every ld_x values; sums: the block's [group][token], this lane's four tokens.
+template <int SIDES, int TILES, int PER_BLOCK, int BLOCKS, int TOKENS>
+__device__ __forceinline__ void int4_block(f32x4 (&acc)[SIDES][TILES], const u32x4 (&w)[SIDES], int u, const uint32_t (&scale_of)[SIDES][Int4Rows<SIDES, BLOCKS, PER_BLOCK>::WORDS],
+                                           const uint32_t (&zero_of)[SIDES][Int4Rows<SIDES, BLOCKS, PER_BLOCK>::ZERO_WORDS], bool zeros,
+                                           const uint16_t *x, int ld_x, const float *sums)
+{
+    f32x4 sum[SIDES][TILES];
+#pragma unroll
+    for (int s = 0; s < 4; s++) {
+        const int in_block = s * PER_BLOCK / 4, i = u * PER_BLOCK + in_block;
+        if (s * PER_BLOCK % 4 == 0) {
+#pragma unroll
+            for (int g = 0; g < SIDES; g++) {
+                const float zero = zeros ? -16.0f - (float)((zero_of[g][i / 4] >> (8 * (i % 4))) & 255u) : -24.0f;
+#pragma unroll
+                for (int t = 0; t < TILES; t++) sum[g][t] = zero * *reinterpret_cast<const f32x4 *>(sums + in_block * TOKENS + 16 * t);
+            }
+        }
+        bf16x8 wf[SIDES];
+#pragma unroll
+        for (int g = 0; g < SIDES; g++) wf[g] = int4_plus16(w[g][s]);
+#pragma unroll
+        for (int t = 0; t < TILES; t++) {
+            const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(x + 16 * t * ld_x + 32 * s);
+#pragma unroll
+            for (int g = 0; g < SIDES; g++) sum[g][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, wf[g], sum[g][t], 0, 0, 0);
+        }
+        if ((s + 1) * PER_BLOCK % 4) continue;
+#pragma unroll
+        for (int g = 0; g < SIDES; g++) {
+            const float scale = half_bits_to_float((uint16_t)(scale_of[g][i / 2] >> (16 * (i % 2))));
 #pragma unroll
             for (int t = 0; t < TILES; t++)
 #pragma unroll
-                for (int g = 0; g < 2; g++) acc[g][t] = (f32x4){0, 0, 0, 0};
-            for (int c0 = 0; c0 < a.blocks; c0 += chunk) {
-                const int n_blocks = min(chunk, a.blocks - c0);
-                const int b0 = c0 + n_blocks * part / a.split, b1 = c0 + n_blocks * (part + 1) / a.split;
-                u32x4 w_next[AHEAD][2];
-                auto load_w = [&](int b) {
+                for (int k = 0; k < 4; k++) acc[g][t][k] = fmaf(scale, sum[g][t][k], acc[g][t][k]);
+        }
+    }
+}
+
+// Results of 16 tokens (of the tile t) and the SIDES tiles of rows from row on; gated: the two are one's gate and product.
+template <int SIDES>
+__device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, const f32x4 (&v)[SIDES], int t, int row, int quarter, int slot0, int ntok)
+{
 #pragma unroll
-                    for (int u = 0; u < AHEAD; u++)
+    for (int k = 0; k < 4; k++) {
+        const int in_tile = 16 * t + 4 * quarter + k;
+        if (in_tile >= ntok) continue;
+        const int token = a.perm ? a.perm[slot0 + in_tile] : slot0 + in_tile;
+        const size_t out_row = a.out_by_slot ? slot0 + in_tile : token;
+        const float gate = a.gate ? a.gate[token] : 1.0f;
+        if (SIDES == 2 && gated) {
+            if (row < a.rows) int4_store(a, out_row, gate, row, int4_gated(v[0][k], v[SIDES - 1][k], a.activation));
+        } else {
 #pragma unroll
-                        for (int g = 0; g < 2; g++) w_next[u][g] = *(gp_u32x4)(w_row[g] + (size_t)64 * max(0, min(b + u, b1 - 1)));
-                };
-                load_w(b0);
-                if (rep == 0 || chunk < a.blocks) {
-                    __syncthreads();  // what lay there before has been read
-                    const int pieces = n_blocks * (kInt4BlockCols / 8);
-                    for (int i = threadIdx.x; i < ntok * pieces; i += blockDim.x) {
-                        const int token = i / pieces, c = 8 * (i - token * pieces), slot = slot0 + token;
-                        const uint16_t *x = a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
-                        const u32x4 v = int4_x(x, kInt4BlockCols * c0 + c, a.cols);
-                        *reinterpret_cast<u32x4 *>(&s_x[token * ld_s + c]) = v;
-                        const float all = int4_group_sum<PER_BLOCK>(v);  // (16 lanes hold a block of a token)
-                        if ((lane + 1) % (16 / PER_BLOCK) == 0) s_sum[(c / (kInt4BlockCols / PER_BLOCK)) * (16 * TILES) + token] = all;
-                    }
-                    __syncthreads();
-                }
-                uint32_t scales[2][WORDS], zeros[2][ZERO_WORDS];  // quarter i: of the i-th step from the last multiple of four on
-                for (int b = b0, it = 0; b < b1; b += AHEAD, it = (it + 1) & 3) {
-                    if (it == 0) {
-                        const int mine = b + AHEAD * quarter, g0 = PER_BLOCK * mine;
-                        if (a.blocks_per_group == 1 && g0 + GROUPS <= a.groups) {
+            for (int g = 0; g < SIDES; g++)
+                if (row + 16 * g < a.rows) int4_store(a, out_row, gate, row + 16 * g, v[g][k]);
+        }
+    }
+}
+
+__device__ __forceinline__ bool int4_gates(const Int4Args &a) { return a.activation == QMOE_ACT_SILU_GATED || a.activation == QMOE_ACT_GELU_GATED; }
+
+struct Int4Unit {
+    int expert, slot0, ntok;
+};
+__device__ __forceinline__ Int4Unit int4_unit(const Int4Args &a, int item, int tokens)
+{
+    if (!a.items) return {0, item * tokens, min(tokens, a.batch - item * tokens)};
+    const Item it = a.items[item];
+    return {it.expert, it.slot0, min(it.ntok, tokens)};
+}
+__device__ __forceinline__ const uint16_t *int4_x_row(const Int4Args &a, int slot)
+{
+    return a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
+}
+
+// Little work: a workgroup's wavefronts share 16 rows (gated: of each projection) along the columns, each with its own piece of LDS for the
+// activations of its block, so that none waits for another before all join their sums, in a fixed order.
+template <int SIDES, int TILES, int PER_BLOCK>
+__global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Args a)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    constexpr int TOKENS = 16 * TILES, LD = kInt4BlockCols + 8;  // (16 lanes' reads, a token each, meet no bank twice)
+    constexpr int X_BYTES = TOKENS * LD * 2, WAVE_BYTES = X_BYTES + 4 * PER_BLOCK * TOKENS;
+    const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n16 = lane & 15, quarter = lane >> 4, from_lane = 4 * (4 * n16 + quarter);
+    uint16_t *s_x = reinterpret_cast<uint16_t *>(smem + part * WAVE_BYTES);
+    float *s_sum = reinterpret_cast<float *>(smem + part * WAVE_BYTES + X_BYTES);
+    f32x4 *joined = reinterpret_cast<f32x4 *>(smem);
+    const bool gated = int4_gates(a);
+    const int row_tiles = (a.rows + 15) / 16;
+    const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
+    const long long total = (long long)n_items * row_tiles;
+    const int b0 = (int)((long long)a.blocks * part / a.split), b1 = (int)((long long)a.blocks * (part + 1) / a.split);
+    for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
+        const int item = (int)(unit / row_tiles), tile = (int)(unit - (long long)item * row_tiles);
+        const Int4Unit it = int4_unit(a, item, TOKENS);
+        const Int4Matrix m = int4_matrix(a, it.expert);
+        Int4Rows<SIDES, 1, PER_BLOCK> rows;
+        int base[SIDES], behind[SIDES];
 #pragma unroll
-                            for (int g = 0; g < 2; g++) {
-                                __builtin_memcpy(scales[g], m.scale + meta[g] + g0, 2 * GROUPS);
-                                if (m.zero) __builtin_memcpy(zeros[g], m.zero + meta[g] + g0, GROUPS);
-                            }
-                        } else {
+        for (int g = 0; g < SIDES; g++) base[g] = 16 * tile, behind[g] = g * a.rows;
+        rows.at(a, m, lane, base, behind);
+        const uint16_t *x_row[4 * TILES];
 #pragma unroll
-                            for (int g = 0; g < 2; g++) {
+        for (int j = 0; j < 4 * TILES; j++)
+            if (4 * j < it.ntok) x_row[j] = int4_x_row(a, it.slot0 + min(4 * j + quarter, it.ntok - 1));
+        u32x4 x_next[4 * TILES];
+        auto load_x = [&](int b) {
 #pragma unroll
-                                for (int i = 0; i < WORDS; i++) scales[g][i] = 0;
+            for (int j = 0; j < 4 * TILES; j++)
+                if (4 * j < it.ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * n16, a.cols);
+        };
+        f32x4 acc[SIDES][TILES];
 #pragma unroll
-                                for (int i = 0; i < ZERO_WORDS; i++) zeros[g][i] = 0;
+        for (int g = 0; g < SIDES; g++)
 #pragma unroll
-                                for (int i = 0; i < GROUPS; i++) {
-                                    const int of = a.blocks_per_group > 1 ? (mine + i) / a.blocks_per_group : g0 + i;
-                                    const size_t at = meta[g] + min(of, a.groups - 1);
-                                    scales[g][i / 2] |= (uint32_t)m.scale[at] << (16 * (i % 2));
-                                    if (m.zero) zeros[g][i / 4] |= (uint32_t)m.zero[at] << (8 * (i % 4));
-                                }
-                            }
-                        }
-                    }
-                    u32x4 w[AHEAD][2];
+            for (int t = 0; t < TILES; t++) acc[g][t] = (f32x4){0, 0, 0, 0};
+        if (b0 < b1) {
+            rows.load(b0, b1 - 1);
+            load_x(b0);
+        }
+        for (int b = b0; b < b1; b++) {
+            const int step = (b - b0) & 3;
+            if (step == 0) rows.load_scales(a, m, quarter, b);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();  // the block before has been read
 #pragma unroll
-                    for (int u = 0; u < AHEAD; u++)
+            for (int j = 0; j < 4 * TILES; j++) {
+                if (4 * j >= it.ntok) continue;
+                *reinterpret_cast<u32x4 *>(&s_x[(4 * j + quarter) * LD + 8 * n16]) = x_next[j];
+                const float all = int4_group_sum<PER_BLOCK>(x_next[j]);
+                if ((n16 + 1) % (16 / PER_BLOCK) == 0) s_sum[(n16 * PER_BLOCK / 16) * TOKENS + 4 * j + quarter] = all;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            u32x4 w[SIDES];
+            uint32_t scale_of[SIDES][decltype(rows)::WORDS], zero_of[SIDES][decltype(rows)::ZERO_WORDS];
 #pragma unroll
-                        for (int g = 0; g < 2; g++)
+            for (int g = 0; g < SIDES; g++) {
 #pragma unroll
-                            for (int s = 0; s < 4; s++) w[u][g][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)w_next[u][g][s]);
-                    load_w(b + AHEAD);
-                    uint32_t scale_of[2][WORDS], zero_of[2][ZERO_WORDS];
-                    const int from_step = 4 * (n16 + 16 * it);
+                for (int s = 0; s < 4; s++) w[g][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)rows.next[0][g][s]);
 #pragma unroll
-                    for (int g = 0; g < 2; g++) {
+                for (int i = 0; i < decltype(rows)::WORDS; i++)
+                    scale_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (n16 + 16 * step), (int)rows.scales[g][i]);
+                if (m.zero) {
 #pragma unroll
-                        for (int i = 0; i < WORDS; i++) scale_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_step, (int)scales[g][i]);
-                        if (m.zero) {
-#pragma unroll
-                            for (int i = 0; i < ZERO_WORDS; i++) zero_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_step, (int)zeros[g][i]);
-                        }
-                    }
-#pragma unroll
-                    for (int u = 0; u < AHEAD; u++) {
-                        if (b + u >= b1) break;
-                        const uint16_t *x_at = s_x + kInt4BlockCols * (b + u - c0) + 8 * quarter;
-                        const float *sum_at = s_sum + PER_BLOCK * (b + u - c0) * (16 * TILES) + 4 * quarter;
-#pragma unroll
-                        for (int s = 0; s < 4; s++) {
-                            const int in_block = s * PER_BLOCK / 4, i = u * PER_BLOCK + in_block;
-                            if (s * PER_BLOCK % 4 == 0) {
-#pragma unroll
-                                for (int g = 0; g < 2; g++) {
-                                    const float zero = m.zero ? -16.0f - (float)((zero_of[g][i / 4] >> (8 * (i % 4))) & 255u) : -24.0f;
-#pragma unroll
-                                    for (int t = 0; t < TILES; t++)
-                                        sum[g][t] = zero * *reinterpret_cast<const f32x4 *>(sum_at + in_block * 16 * TILES + 16 * t);
-                                }
-                            }
-                            const bf16x8 w0 = int4_plus16(w[u][0][s]), w1 = int4_plus16(w[u][1][s]);
-#pragma unroll
-                            for (int t = 0; t < TILES; t++) {
-                                const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(x_at + min(16 * t + n16, ntok - 1) * ld_s + 32 * s);
-                                sum[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w0, sum[0][t], 0, 0, 0);
-                                sum[1][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w1, sum[1][t], 0, 0, 0);
-                            }
-                            if ((s + 1) * PER_BLOCK % 4) continue;
-#pragma unroll
-                            for (int g = 0; g < 2; g++) {
-                                const float scale = half_bits_to_float((uint16_t)(scale_of[g][i / 2] >> (16 * (i % 2))));
-#pragma unroll
-                                for (int t = 0; t < TILES; t++)
-#pragma unroll
-                                    for (int k = 0; k < 4; k++) acc[g][t][k] = fmaf(scale, sum[g][t][k], acc[g][t][k]);
-                            }
-                        }
-                    }
+                    for (int i = 0; i < decltype(rows)::ZERO_WORDS; i++)
+                        zero_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (n16 + 16 * step), (int)rows.zeros[g][i]);
                 }
             }
-            f32x4 *mine = joined + (size_t)(in_group * a.split) * 2 * TILES * 64;
-            if (a.split > 1) {
+            if (b + 1 < b1) {
+                rows.load(b + 1, b1 - 1);
+                load_x(b + 1);
+            }
+            int4_block<SIDES, TILES, PER_BLOCK, 1, TOKENS>(acc, w, 0, scale_of, zero_of, m.zero != nullptr, s_x + n16 * LD + 8 * quarter, LD,
+                                                           s_sum + 4 * quarter);
+        }
+        __syncthreads();  // all have read their activations: the sums take their place
 #pragma unroll
-                for (int g = 0; g < 2; g++)
+        for (int g = 0; g < SIDES; g++)
 #pragma unroll
-                    for (int t = 0; t < TILES; t++) mine[((part * 2 + g) * TILES + t) * 64 + lane] = acc[g][t];
-                __syncthreads();
+            for (int t = 0; t < TILES; t++) joined[((part * SIDES + g) * TILES + t) * 64 + lane] = acc[g][t];
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TILES; t++) {
+            if (t % a.split != part || 16 * t >= it.ntok) continue;  // a tile of tokens is joined by one of the wavefronts
+            f32x4 v[SIDES];
+#pragma unroll
+            for (int g = 0; g < SIDES; g++) {
+                v[g] = joined[(g * TILES + t) * 64 + lane];
+                for (int p = 1; p < a.split; p++) v[g] += joined[((p * SIDES + g) * TILES + t) * 64 + lane];
+            }
+            int4_results<SIDES>(a, gated, v, t, 16 * tile + n16, quarter, it.slot0, it.ntok);
+        }
+        __syncthreads();  // before the next unit's activations overwrite these
+    }
+}
+
+// More work: four wavefronts with two tiles of 16 rows each (gated: the same rows of both projections) and all the columns.  Steps of
+// two blocks: the activations of the next one and a wavefront's weights are on their way while this one is multiplied; x
+// goes through LDS in two turns, a barrier a step.
+template <int TILES, int PER_BLOCK>
+__global__ __launch_bounds__(256, TILES == 1 ? 4 : 2) void k_int4_tile(const Int4Args a)
+{
+    constexpr int TOKENS = 16 * TILES, BLOCKS = 2, COLS = BLOCKS * kInt4BlockCols, LD = COLS + 8;
+    __shared__ __align__(16) uint16_t s_x[2][TOKENS * LD];
+    __shared__ __align__(16) float s_sum[2][BLOCKS * PER_BLOCK * TOKENS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n16 = lane & 15, quarter = lane >> 4, from_lane = 4 * (4 * n16 + quarter);
+    const int piece = threadIdx.x & 31, stager = threadIdx.x >> 5;  // brings 8 columns of tokens stager + 8 j
+    const bool gated = int4_gates(a);
+    const int wave_rows = gated ? 16 : 32, units_per_item = (a.rows + 4 * wave_rows - 1) / (4 * wave_rows);
+    const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
+    const long long total = (long long)n_items * units_per_item;
+    for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
+        const int item = (int)(unit / units_per_item), first = ((int)(unit - (long long)item * units_per_item) * 4 + wave) * wave_rows;
+        const Int4Unit it = int4_unit(a, item, TOKENS);
+        const Int4Matrix m = int4_matrix(a, it.expert);
+        Int4Rows<2, BLOCKS, PER_BLOCK> rows;
+        rows.at(a, m, lane, {first, gated ? first : first + 16}, {0, gated ? a.rows : 0});
+        rows.load(0, a.blocks - 1);
+        const uint16_t *x_row[2 * TILES];
+#pragma unroll
+        for (int j = 0; j < 2 * TILES; j++)
+            if (8 * j < it.ntok) x_row[j] = int4_x_row(a, it.slot0 + min(8 * j + stager, it.ntok - 1));
+        u32x4 x_next[2 * TILES];
+        auto load_x = [&](int b) {
+#pragma unroll
+            for (int j = 0; j < 2 * TILES; j++)
+                if (8 * j < it.ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * piece, a.cols);
+        };
+        load_x(0);
+        f32x4 acc[2][TILES];
+#pragma unroll
+        for (int g = 0; g < 2; g++)
+#pragma unroll
+            for (int t = 0; t < TILES; t++) acc[g][t] = (f32x4){0, 0, 0, 0};
+        __syncthreads();  // the unit before has read its last steps
+        for (int b = 0, turn = 0, step = 0; b < a.blocks; b += BLOCKS, turn ^= 1, step = (step + 1) & 3) {
+            if (step == 0) rows.load_scales(a, m, quarter, b);
+#pragma unroll
+            for (int j = 0; j < 2 * TILES; j++) {
+                if (8 * j >= it.ntok) continue;
+                const int token = 8 * j + stager;
+                *reinterpret_cast<u32x4 *>(&s_x[turn][token * LD + 8 * piece]) = x_next[j];
+                const float all = int4_group_sum<PER_BLOCK>(x_next[j]);
+                if ((piece + 1) % (16 / PER_BLOCK) == 0) s_sum[turn][(piece * PER_BLOCK / 16) * TOKENS + token] = all;
+            }
+            __syncthreads();
+            u32x4 w[BLOCKS][2];
+            uint32_t scale_of[2][decltype(rows)::WORDS], zero_of[2][decltype(rows)::ZERO_WORDS];
+#pragma unroll
+            for (int g = 0; g < 2; g++) {
+#pragma unroll
+                for (int u = 0; u < BLOCKS; u++)
+#pragma unroll
+                    for (int s = 0; s < 4; s++) w[u][g][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)rows.next[u][g][s]);
+#pragma unroll
+                for (int i = 0; i < decltype(rows)::WORDS; i++)
+                    scale_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (n16 + 16 * step), (int)rows.scales[g][i]);
+                if (m.zero) {
+#pragma unroll
+                    for (int i = 0; i < decltype(rows)::ZERO_WORDS; i++)
+                        zero_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (n16 + 16 * step), (int)rows.zeros[g][i]);
+                }
+            }
+            if (b + BLOCKS < a.blocks) {
+                rows.load(b + BLOCKS, a.blocks - 1);
+                load_x(b + BLOCKS);
             }
 #pragma unroll
-            for (int t = 0; t < TILES; t++) {
-                if (t % a.split != part) continue;  // a tile of tokens is joined by one of the wavefronts
-                if (16 * t >= ntok) break;
-                if (a.split > 1) {
-#pragma unroll
-                    for (int g = 0; g < 2; g++) {
-                        f32x4 v = mine[(g * TILES + t) * 64 + lane];
-                        for (int p = 1; p < a.split; p++) v += mine[((p * 2 + g) * TILES + t) * 64 + lane];
-                        acc[g][t] = v;
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const int in_tile = 16 * t + 4 * quarter + k;
-                    if (in_tile >= ntok) continue;
-                    const int token = a.perm ? a.perm[slot0 + in_tile] : slot0 + in_tile;
-                    const size_t out_row = a.out_by_slot ? slot0 + in_tile : token;
-                    const float gate = a.gate ? a.gate[token] : 1.0f;
-                    const int r = unit_rows * tile + n16;
-                    if (gated) {
-                        if (r < a.rows) int4_store(a, out_row, gate, r, int4_gated(acc[0][t][k], acc[1][t][k], a.activation));
-                    } else {
-                        if (r < a.rows) int4_store(a, out_row, gate, r, acc[0][t][k]);
-                        if (r + 16 < a.rows) int4_store(a, out_row, gate, r + 16, acc[1][t][k]);
-                    }
-                }
+            for (int u = 0; u < BLOCKS; u++) {
+                if (b + u >= a.blocks) break;
+                int4_block<2, TILES, PER_BLOCK, BLOCKS, TOKENS>(acc, w[u], u, scale_of, zero_of, m.zero != nullptr,
+                                                                s_x[turn] + n16 * LD + kInt4BlockCols * u + 8 * quarter, LD,
+                                                                s_sum[turn] + u * PER_BLOCK * TOKENS + 4 * quarter);
             }
-            if (a.split > 1) __syncthreads();  // before the next tile's sums overwrite these
+        }
+#pragma unroll
+        for (int t = 0; t < TILES; t++) {
+            if (16 * t >= it.ntok) break;
+            const f32x4 v[2] = {acc[0][t], acc[1][t]};
+            int4_results<2>(a, gated, v, t, first + n16, quarter, it.slot0, it.ntok);
         }
     }
 }
@@ -228,45 +355,56 @@ void fill_shape(Int4Args *a, int rows, int cols, int group)
     a->blocks_per_group = group < kInt4BlockCols ? 1 : group / kInt4BlockCols;
 }
 
-template <int TILES, int PER_BLOCK>
-qmoe_status launch_rows_variant(const Int4Args &a, int grid, int threads, hipStream_t s)
+template <int SIDES, int TILES, int PER_BLOCK>
+qmoe_status launch_split_variant(const Int4Args &a, int grid, hipStream_t s)
 {
-    const size_t smem = a.x_bytes + a.sum_bytes + (a.split > 1 ? (size_t)(threads / 64) * 2 * TILES * 64 * sizeof(f32x4) : 0);
-    const qmoe_status st = allow_lds(k_int4_rows<TILES, PER_BLOCK>, smem);
+    const size_t tokens = 16 * TILES, x = a.split * (tokens * (kInt4BlockCols + 8) * 2 + 4 * PER_BLOCK * tokens);
+    const size_t smem = std::max(x, (size_t)a.split * SIDES * TILES * 64 * sizeof(f32x4));
+    const qmoe_status st = allow_lds(k_int4_split<SIDES, TILES, PER_BLOCK>, smem);
     if (st != QMOE_OK) return st;
-    hipLaunchKernelGGL((k_int4_rows<TILES, PER_BLOCK>), dim3(grid), dim3(threads), smem, s, a);
+    hipLaunchKernelGGL((k_int4_split<SIDES, TILES, PER_BLOCK>), dim3(grid), dim3(64 * a.split), smem, s, a);
+    QMOE_HIP_TRY(hipGetLastError());
+    return QMOE_OK;
+}
+template <int SIDES, int TILES>
+qmoe_status launch_split_tiles(const Int4Args &a, int grid, hipStream_t s)
+{
+    if (a.per_block == 1) return launch_split_variant<SIDES, TILES, 1>(a, grid, s);
+    if (a.per_block == 2) return launch_split_variant<SIDES, TILES, 2>(a, grid, s);
+    return launch_split_variant<SIDES, TILES, 4>(a, grid, s);
+}
+template <int SIDES>
+qmoe_status launch_split_sides(const Int4Args &a, int tiles, int grid, hipStream_t s)
+{
+    if (tiles <= 1) return launch_split_tiles<SIDES, 1>(a, grid, s);
+    if (tiles <= 2) return launch_split_tiles<SIDES, 2>(a, grid, s);
+    return launch_split_tiles<SIDES, 4>(a, grid, s);
+}
+template <int TILES>
+qmoe_status launch_tile_variant(const Int4Args &a, int grid, hipStream_t s)
+{
+    if (a.per_block == 1) hipLaunchKernelGGL((k_int4_tile<TILES, 1>), dim3(grid), dim3(256), 0, s, a);
+    else if (a.per_block == 2) hipLaunchKernelGGL((k_int4_tile<TILES, 2>), dim3(grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_int4_tile<TILES, 4>), dim3(grid), dim3(256), 0, s, a);
     QMOE_HIP_TRY(hipGetLastError());
     return QMOE_OK;
 }
 
 // tiles: tiles of 16 tokens of an item; items: how many the call has, about
-qmoe_status launch_rows_kernel(Int4Args a, int tiles, long long items, int cus, hipStream_t s)
+qmoe_status launch_few(Int4Args a, int tiles, long long items, int cus, hipStream_t s)
 {
-    const int unit_rows = int4_is_gated(a.activation) ? 16 : 32, row_tiles = (a.rows + unit_rows - 1) / unit_rows;
-    const long long units = items * row_tiles;
-    a.split = 1;
-    while (a.split < kInt4MaxSplit && units * a.split < 8LL * cus && 2 * a.split <= a.blocks) a.split *= 2;
-    const int threads = 64 * (a.split < 4 ? 4 : a.split);
-    const int side_by_side = threads / 64 / a.split;
-    // several tiles a wavefront where that leaves enough workgroups: the activations are staged once for them
-    a.reps = (int)std::min<long long>(2, std::max<long long>(1, items * row_tiles / (16LL * cus * side_by_side)));
-    const long long groups = items * ((row_tiles + side_by_side * a.reps - 1) / (side_by_side * a.reps));
-    const int tokens = 16 * (tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4);
-    a.x_bytes = (uint32_t)std::min<size_t>(kInt4XBytes, (size_t)tokens * 2 * (a.blocks * kInt4BlockCols + 8));
-    const int grid = (int)std::min<long long>(groups, 64LL * cus);
-    a.sum_bytes = (uint32_t)std::min<size_t>(kInt4XBytes / 4, (size_t)tokens * 4 * a.blocks * a.per_block);
-    const int variant = (tiles <= 1 ? 0 : tiles <= 2 ? 3 : 6) + (a.per_block == 1 ? 0 : a.per_block == 2 ? 1 : 2);
-    switch (variant) {
-    case 0: return launch_rows_variant<1, 1>(a, grid, threads, s);
-    case 1: return launch_rows_variant<1, 2>(a, grid, threads, s);
-    case 2: return launch_rows_variant<1, 4>(a, grid, threads, s);
-    case 3: return launch_rows_variant<2, 1>(a, grid, threads, s);
-    case 4: return launch_rows_variant<2, 2>(a, grid, threads, s);
-    case 5: return launch_rows_variant<2, 4>(a, grid, threads, s);
-    case 6: return launch_rows_variant<4, 1>(a, grid, threads, s);
-    case 7: return launch_rows_variant<4, 2>(a, grid, threads, s);
-    default: return launch_rows_variant<4, 4>(a, grid, threads, s);
+    const bool gated = int4_is_gated(a.activation);
+    const long long row_tiles = (a.rows + 15) / 16, tile_units = items * ((a.rows + (gated ? 63 : 127)) / (gated ? 64 : 128));
+    if (tile_units < 2LL * cus) {
+        a.split = 1;
+        while (a.split < kInt4MaxSplit && a.split < a.blocks && items * row_tiles * a.split < 16LL * cus) a.split *= 2;
+        const int grid = (int)std::min<long long>(items * row_tiles, 32LL * cus);
+        return gated ? launch_split_sides<2>(a, tiles, grid, s) : launch_split_sides<1>(a, tiles, grid, s);
     }
+    const int grid = (int)std::min<long long>(tile_units, 64LL * cus);
+    if (tiles <= 1) return launch_tile_variant<1>(a, grid, s);
+    if (tiles <= 2) return launch_tile_variant<2>(a, grid, s);
+    return launch_tile_variant<4>(a, grid, s);
 }
 
 // zeros: a matrix has zero points (descriptors in device memory: may have)
@@ -310,7 +448,7 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W, const uint16_t *x_bf16, 
     fill_shape(&a, rows, W->cols, W->group);
     if (batch > 64) return launch_mm_kernel(a, a.zero != nullptr, di.cus, static_cast<hipStream_t>(stream));
     const int tiles = (batch + 15) / 16, at_once = tiles <= 2 ? tiles : 4;
-    return launch_rows_kernel(a, tiles, (tiles + at_once - 1) / at_once, di.cus, static_cast<hipStream_t>(stream));
+    return launch_few(a, tiles, (tiles + at_once - 1) / at_once, di.cus, static_cast<hipStream_t>(stream));
 }
 
 qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_matrix *wo, int group, int activation, int n_experts,
@@ -347,12 +485,12 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
         a.items = g.few;
         a.n_items_dev = g.n_few;
         a.max_items = std::min(n_tokens, n_experts + n_tokens / kInt4FewTokens);
-        qmoe_status r = launch_rows_kernel(a, 1, a.max_items, di.cus, s);
+        qmoe_status r = launch_few(a, 1, a.max_items, di.cus, s);
         if (r != QMOE_OK || !crowded) return r;
         a.items = g.many;
         a.n_items_dev = g.n_many;
         a.max_items = n_tokens / kInt4FewTokens;  // (each has more than that, or stands beside a whole tile)
-        return launch_mm_kernel(a, true, di.cus, s);
+        return launch_few(a, 4, a.max_items, di.cus, s);
     };
     if ((st = product()) != QMOE_OK) return st;
     a.mats = wo;

@@ -173,7 +173,7 @@ qmoe_status launch_shape(const Int4Args &a, long long items, int cus, hipStream_
 template <bool GATED, bool ZEROS>
 qmoe_status launch_mm(const Int4Args &a, int cus, hipStream_t s)
 {
-    if (a.items) return launch_shape<4, 4, GATED, ZEROS>(a, a.max_items, cus, s);
+    if (a.items) return launch_shape<2, 4, GATED, ZEROS>(a, a.max_items, cus, s);
     const long long tiles128 = (a.batch + 127) / 128, blocks = (a.rows + (GATED ? 127 : 255)) / (GATED ? 128 : 256);
     if (tiles128 * blocks >= cus) return launch_shape<4, 8, GATED, ZEROS>(a, tiles128, cus, s);
     const long long tiles64 = (a.batch + 63) / 64;
