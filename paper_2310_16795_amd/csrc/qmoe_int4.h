@@ -29,17 +29,45 @@ struct Int4Args {
     int split;                     // k_int4_split: wavefronts that share a tile of rows along the columns
 };
 
-// One matrix as a wavefront reads it.
+// One matrix as a wavefront reads it.  Its pointers may come out of an array in memory, so they are given their address space by
+// hand: through a generic pointer every load would also count as LDS traffic and be waited for together with it.
+using gp_bytes = const __attribute__((address_space(1))) uint8_t *;
+using gp_u16 = const __attribute__((address_space(1))) uint16_t *;
 struct Int4Matrix {
     const uint8_t *weights;
-    const uint16_t *scale;
-    const uint8_t *zero;
+    gp_u16 scale;
+    gp_bytes zero;
 };
 __device__ __forceinline__ Int4Matrix int4_matrix(const Int4Args &a, int expert)
 {
-    if (!a.mats) return {a.weights, a.scale, a.zero};
+    if (!a.mats) return {a.weights, (gp_u16)a.scale, (gp_bytes)a.zero};
     const qmoe_int4_matrix &m = a.mats[expert];
-    return {m.weights, m.scale_f16, m.zero};
+    return {m.weights, (gp_u16)m.scale_f16, (gp_bytes)m.zero};
+}
+// N values of 2 or 1 bytes from memory, in N / 2 or N / 4 words
+template <int BYTES> struct Int4Packed;
+typedef uint16_t u16_by1 __attribute__((aligned(1)));
+typedef uint32_t u32_by1 __attribute__((aligned(1)));
+typedef uint32_t u32x2_by1 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32x4_by1 __attribute__((ext_vector_type(4), aligned(1)));
+template <> struct Int4Packed<2> { using at = const __attribute__((address_space(1))) u16_by1 *; };
+template <> struct Int4Packed<4> { using at = const __attribute__((address_space(1))) u32_by1 *; };
+template <> struct Int4Packed<8> { using at = const __attribute__((address_space(1))) u32x2_by1 *; };
+template <> struct Int4Packed<16> { using at = const __attribute__((address_space(1))) u32x4_by1 *; };
+template <int BYTES, int WORDS, typename P>
+__device__ __forceinline__ void int4_load_packed(uint32_t (&v)[WORDS], P from)
+{
+    if constexpr (BYTES == 1) {
+        v[0] = *from;
+    } else {
+        const auto w = *(typename Int4Packed<BYTES>::at)from;
+        if constexpr (BYTES <= 4) {
+            v[0] = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; i++) v[i] = w[i];
+        }
+    }
 }
 
 // Eight weights (a word) as bf16 16 + q, in the order of their columns: bits 3..6 of a bf16 between 16 and 32 are its
@@ -54,14 +82,34 @@ __device__ __forceinline__ bf16x8 int4_plus16(uint32_t w)
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// Eight activations of a token from column c on, 0 from column cols on.
-__device__ __forceinline__ u32x4 int4_x(const uint16_t *row, int c, int cols)
+// Eight activations of a token from column c on, 0 from column cols on.  whole: none is missing (the same for the wavefront).  The other
+// path is rare, and is kept from asking for registers that the loop around it needs.
+__device__ __forceinline__ u32x4 int4_x(const uint16_t *row, int c, int cols, bool whole)
 {
-    if (c + 8 <= cols) return *reinterpret_cast<const u32x4_by2 *>(row + c);
+    if (whole) return *reinterpret_cast<const u32x4_by2 *>(row + c);
     u32x4 v = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; i++)
+    for (int i = 0; i < 8; i++) {
         if (c + i < cols) v[i / 2] |= (uint32_t)row[c + i] << (16 * (i % 2));
+        asm volatile("" ::: "memory");
+    }
+    return v;
+}
+
+// The same in two parts, for loops that keep loads on their way (a branch with loads of its own would have them all waited for): eight
+// values from column c on or from the row's last eight (cols >= 8) ...
+__device__ __forceinline__ u32x4 int4_x_load(const uint16_t *row, int c, int cols)
+{
+    return *reinterpret_cast<const u32x4_by2 *>(row + min(c, cols - 8));
+}
+// ... and, where the row ends in them, those from c on moved to the front, zeros behind.
+__device__ __forceinline__ u32x4 int4_x_end(u32x4 v, int c, int cols)
+{
+    const int over = max(0, min(c + 8 - cols, 8));
+    if (over & 1) v = (u32x4){v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+    if (over & 2) v = (u32x4){v[1], v[2], v[3], 0u};
+    if (over & 4) v = (u32x4){v[2], v[3], 0u, 0u};
+    if (over & 8) v = (u32x4){0u, 0u, 0u, 0u};
     return v;
 }
 

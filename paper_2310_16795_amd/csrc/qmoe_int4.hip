@@ -24,7 +24,6 @@ struct Int4Rows {
     static constexpr int GROUPS = BLOCKS * PER_BLOCK, WORDS = (GROUPS + 1) / 2, ZERO_WORDS = (GROUPS + 3) / 4;
     const uint8_t *row[SIDES];
     size_t meta[SIDES];
-    u32x4 next[BLOCKS][SIDES];
     uint32_t scales[SIDES][WORDS], zeros[SIDES][ZERO_WORDS];
 
     // the tile's first row on each side, and what stands behind it in the matrix (the other projection)
@@ -37,7 +36,7 @@ struct Int4Rows {
             meta[g] = (size_t)(min(base[g] + (lane & 15), a.rows - 1) + behind[g]) * a.groups;
         }
     }
-    __device__ __forceinline__ void load(int b, int last)
+    __device__ __forceinline__ void load(u32x4 (&next)[BLOCKS][SIDES], int b, int last) const
     {
 #pragma unroll
         for (int u = 0; u < BLOCKS; u++)
@@ -51,8 +50,8 @@ struct Int4Rows {
         if (a.blocks_per_group == 1 && g0 + GROUPS <= a.groups) {
 #pragma unroll
             for (int g = 0; g < SIDES; g++) {
-                __builtin_memcpy(scales[g], m.scale + meta[g] + g0, 2 * GROUPS);
-                if (m.zero) __builtin_memcpy(zeros[g], m.zero + meta[g] + g0, GROUPS);
+                int4_load_packed<2 * GROUPS>(scales[g], m.scale + (meta[g] + g0));
+                if (m.zero) int4_load_packed<GROUPS>(zeros[g], m.zero + (meta[g] + g0));
             }
             return;
         }
@@ -68,6 +67,7 @@ struct Int4Rows {
                 const size_t at = meta[g] + min(of, a.groups - 1);
                 scales[g][i / 2] |= (uint32_t)m.scale[at] << (16 * (i % 2));
                 if (m.zero) zeros[g][i / 4] |= (uint32_t)m.zero[at] << (8 * (i % 4));
+                asm volatile("" ::: "memory");  // (rare: kept from asking for registers that the loop around it needs)
             }
         }
     }
@@ -181,11 +181,11 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 #pragma unroll
         for (int j = 0; j < 4 * TILES; j++)
             if (4 * j < it.ntok) x_row[j] = int4_x_row(a, it.slot0 + min(4 * j + quarter, it.ntok - 1));
-        u32x4 x_next[4 * TILES];
+        u32x4 x_next[4 * TILES], w_next[1][SIDES];
         auto load_x = [&](int b) {
 #pragma unroll
             for (int j = 0; j < 4 * TILES; j++)
-                if (4 * j < it.ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * n16, a.cols);
+                if (4 * j < it.ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * n16, a.cols, kInt4BlockCols * (b + 1) <= a.cols);
         };
         f32x4 acc[SIDES][TILES];
 #pragma unroll
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 #pragma unroll
             for (int t = 0; t < TILES; t++) acc[g][t] = (f32x4){0, 0, 0, 0};
         if (b0 < b1) {
-            rows.load(b0, b1 - 1);
+            rows.load(w_next, b0, b1 - 1);
             load_x(b0);
         }
         for (int b = b0; b < b1; b++) {
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 #pragma unroll
             for (int g = 0; g < SIDES; g++) {
 #pragma unroll
-                for (int s = 0; s < 4; s++) w[g][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)rows.next[0][g][s]);
+                for (int s = 0; s < 4; s++) w[g][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)w_next[0][g][s]);
 #pragma unroll
                 for (int i = 0; i < decltype(rows)::WORDS; i++)
                     scale_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (n16 + 16 * step), (int)rows.scales[g][i]);
@@ -226,10 +226,10 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
                 }
             }
             if (b + 1 < b1) {
-                rows.load(b + 1, b1 - 1);
+                rows.load(w_next, b + 1, b1 - 1);
                 load_x(b + 1);
             }
-            int4_block<SIDES, TILES, PER_BLOCK, 1, TOKENS>(acc, w, 0, scale_of, zero_of, m.zero != nullptr, s_x + n16 * LD + 8 * quarter, LD,
+            int4_block<SIDES, TILES, PER_BLOCK, 1, TOKENS>(acc, w, 0, scale_of, zero_of, bool(m.zero), s_x + n16 * LD + 8 * quarter, LD,
                                                            s_sum + 4 * quarter);
         }
         __syncthreads();  // all have read their activations: the sums take their place
@@ -255,16 +255,22 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 
 // More work: four wavefronts with two tiles of 16 rows each (gated: the same rows of both projections) and all the columns.  Steps of
 // two blocks: the activations of the next one and a wavefront's weights are on their way while this one is multiplied; x
-// goes through LDS in two turns, a barrier a step.
+// goes through LDS in two turns, a barrier a step.  Up to four tokens each wavefront brings for itself, into a quarter of that LDS, and none waits for
+// another.
+// The scales and zero points of AT_ONCE groups go through LDS, too, a wavefront's own: a row's few bytes a step, asked for step by step, would
+// be the same lines of memory again and again, gone from the caches in between.
 template <int TILES, int PER_BLOCK>
 __global__ __launch_bounds__(256, TILES == 1 ? 4 : 2) void k_int4_tile(const Int4Args a)
 {
-    constexpr int TOKENS = 16 * TILES, BLOCKS = 2, COLS = BLOCKS * kInt4BlockCols, LD = COLS + 8;
+    constexpr int TOKENS = 16 * TILES, BLOCKS = 2, COLS = BLOCKS * kInt4BlockCols, LD = COLS + 8, GROUPS = BLOCKS * PER_BLOCK;
+    constexpr int AT_ONCE = TILES == 4 ? 16 : 32, LD_SCALE = AT_ONCE + 8, LD_ZERO = AT_ONCE + 8;
+    using Rows = Int4Rows<2, BLOCKS, PER_BLOCK>;
     __shared__ __align__(16) uint16_t s_x[2][TOKENS * LD];
     __shared__ __align__(16) float s_sum[2][BLOCKS * PER_BLOCK * TOKENS];
+    __shared__ __align__(16) uint16_t s_scale[4][2 * 16 * LD_SCALE];
+    __shared__ __align__(16) uint8_t s_zero[4][2 * 16 * LD_ZERO];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n16 = lane & 15, quarter = lane >> 4, from_lane = 4 * (4 * n16 + quarter);
-    const int piece = threadIdx.x & 31, stager = threadIdx.x >> 5;  // brings 8 columns of tokens stager + 8 j
     const bool gated = int4_gates(a);
     const int wave_rows = gated ? 16 : 32, units_per_item = (a.rows + 4 * wave_rows - 1) / (4 * wave_rows);
     const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
@@ -273,65 +279,114 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 2) void k_int4_tile(const Int
         const int item = (int)(unit / units_per_item), first = ((int)(unit - (long long)item * units_per_item) * 4 + wave) * wave_rows;
         const Int4Unit it = int4_unit(a, item, TOKENS);
         const Int4Matrix m = int4_matrix(a, it.expert);
-        Int4Rows<2, BLOCKS, PER_BLOCK> rows;
+        Rows rows;
         rows.at(a, m, lane, {first, gated ? first : first + 16}, {0, gated ? a.rows : 0});
-        rows.load(0, a.blocks - 1);
+        const bool alone = TILES == 1 && it.ntok <= 4;
+        const int piece = threadIdx.x & 31, stager = alone ? lane >> 5 : threadIdx.x >> 5, stagers = alone ? 2 : 8;
+        const int place = alone ? 4 * wave : 0;  // of the tile's first token in LDS
         const uint16_t *x_row[2 * TILES];
 #pragma unroll
         for (int j = 0; j < 2 * TILES; j++)
-            if (8 * j < it.ntok) x_row[j] = int4_x_row(a, it.slot0 + min(8 * j + stager, it.ntok - 1));
+            x_row[j] = int4_x_row(a, it.slot0 + min(stagers * j + stager, it.ntok - 1));
         u32x4 x_next[2 * TILES];
         auto load_x = [&](int b) {
 #pragma unroll
-            for (int j = 0; j < 2 * TILES; j++)
-                if (8 * j < it.ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * piece, a.cols);
+            for (int j = 0; j < 2 * TILES; j++) x_next[j] = int4_x_load(x_row[j], kInt4BlockCols * b + 8 * piece, a.cols);
         };
+        u32x4 w_next[BLOCKS][2];
+        rows.load(w_next, 0, a.blocks - 1);
         load_x(0);
+        // groups g0 .. g0 + AT_ONCE - 1 of the wavefront's 32 rows: eight lanes a row, eight groups a lane
+        auto fill = [&](int g0) {
+            constexpr int LANES = AT_ONCE / 8, AT = 64 / LANES;  // lanes of a row, rows at a time
+#pragma unroll
+            for (int j = 0; j < 32 / AT; j++) {
+                const int r = AT * j + lane / LANES, at = 8 * (lane % LANES), side = r >> 4;
+                const int base = gated ? first : first + 16 * side;
+                const size_t row = (size_t)(min(base + (r & 15), a.rows - 1) + (gated ? side * a.rows : 0)) * a.groups;
+                uint16_t *to = &s_scale[wave][r * LD_SCALE + at];
+                uint8_t *to_zero = &s_zero[wave][r * LD_ZERO + at];
+                if (g0 + at + 8 <= a.groups) {
+                    uint32_t v[4], z[2] = {0x08080808u, 0x08080808u};
+                    int4_load_packed<16>(v, m.scale + (row + g0 + at));
+                    if (m.zero) int4_load_packed<8>(z, m.zero + (row + g0 + at));
+                    *reinterpret_cast<u32x4 *>(to) = (u32x4){v[0], v[1], v[2], v[3]};
+                    *reinterpret_cast<uint2 *>(to_zero) = make_uint2(z[0], z[1]);
+                } else {
+                    for (int i = 0; i < 8; i++) {  // 0 behind the last group: its columns are none, but what lies there could be infinite
+                        const bool is = g0 + at + i < a.groups;
+                        to[i] = is ? m.scale[row + g0 + at + i] : 0;
+                        to_zero[i] = is && m.zero ? m.zero[row + g0 + at + i] : 8;
+                    }
+                }
+            }
+        };
         f32x4 acc[2][TILES];
 #pragma unroll
         for (int g = 0; g < 2; g++)
 #pragma unroll
             for (int t = 0; t < TILES; t++) acc[g][t] = (f32x4){0, 0, 0, 0};
         __syncthreads();  // the unit before has read its last steps
-        for (int b = 0, turn = 0, step = 0; b < a.blocks; b += BLOCKS, turn ^= 1, step = (step + 1) & 3) {
-            if (step == 0) rows.load_scales(a, m, quarter, b);
+        const int x_at = (place + (alone ? n16 & 3 : n16)) * LD + 8 * quarter, sum_at = alone ? place : 4 * quarter;
+        const int last_step = (a.blocks - 1) / BLOCKS * BLOCKS;
+        auto one_step = [&](int b, int g_from, int turn) {
+            if (kInt4BlockCols * b + COLS > a.cols) {
+#pragma unroll
+                for (int j = 0; j < 2 * TILES; j++) x_next[j] = int4_x_end(x_next[j], kInt4BlockCols * b + 8 * piece, a.cols);
+            }
 #pragma unroll
             for (int j = 0; j < 2 * TILES; j++) {
-                if (8 * j >= it.ntok) continue;
-                const int token = 8 * j + stager;
+                if (alone && j > 1) break;
+                const int token = place + stagers * j + stager;
                 *reinterpret_cast<u32x4 *>(&s_x[turn][token * LD + 8 * piece]) = x_next[j];
                 const float all = int4_group_sum<PER_BLOCK>(x_next[j]);
                 if ((piece + 1) % (16 / PER_BLOCK) == 0) s_sum[turn][(piece * PER_BLOCK / 16) * TOKENS + token] = all;
             }
-            __syncthreads();
+            if (alone) {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            } else {
+                __syncthreads();
+            }
             u32x4 w[BLOCKS][2];
-            uint32_t scale_of[2][decltype(rows)::WORDS], zero_of[2][decltype(rows)::ZERO_WORDS];
+            uint32_t scale_of[2][Rows::WORDS], zero_of[2][Rows::ZERO_WORDS];
+            // the step's groups, from the first that lies in LDS on
+            const int from = (a.blocks_per_group > 1 ? b / a.blocks_per_group : b * PER_BLOCK) - g_from;
 #pragma unroll
             for (int g = 0; g < 2; g++) {
 #pragma unroll
                 for (int u = 0; u < BLOCKS; u++)
 #pragma unroll
-                    for (int s = 0; s < 4; s++) w[u][g][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)rows.next[u][g][s]);
-#pragma unroll
-                for (int i = 0; i < decltype(rows)::WORDS; i++)
-                    scale_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (n16 + 16 * step), (int)rows.scales[g][i]);
-                if (m.zero) {
-#pragma unroll
-                    for (int i = 0; i < decltype(rows)::ZERO_WORDS; i++)
-                        zero_of[g][i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (n16 + 16 * step), (int)rows.zeros[g][i]);
+                    for (int s = 0; s < 4; s++) w[u][g][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)w_next[u][g][s]);
+                const int r = 16 * g + n16;
+                const uint16_t *scale = &s_scale[wave][r * LD_SCALE];
+                const uint8_t *zero = &s_zero[wave][r * LD_ZERO];
+                if constexpr (PER_BLOCK == 1) {
+                    const int then = (a.blocks_per_group > 1 ? (b + 1) / a.blocks_per_group : b + 1) - g_from;
+                    scale_of[g][0] = (uint32_t)scale[from] | (uint32_t)scale[then] << 16;
+                    zero_of[g][0] = (uint32_t)zero[from] | (uint32_t)zero[then] << 8;
+                } else {
+                    __builtin_memcpy(scale_of[g], __builtin_assume_aligned(scale + from, 2 * GROUPS), 2 * GROUPS);
+                    __builtin_memcpy(zero_of[g], __builtin_assume_aligned(zero + from, GROUPS), GROUPS);
                 }
             }
-            if (b + BLOCKS < a.blocks) {
-                rows.load(b + BLOCKS, a.blocks - 1);
-                load_x(b + BLOCKS);
-            }
+            rows.load(w_next, b + BLOCKS, a.blocks - 1);
+            load_x(min(b + BLOCKS, last_step));
 #pragma unroll
             for (int u = 0; u < BLOCKS; u++) {
                 if (b + u >= a.blocks) break;
-                int4_block<2, TILES, PER_BLOCK, BLOCKS, TOKENS>(acc, w[u], u, scale_of, zero_of, m.zero != nullptr,
-                                                                s_x[turn] + n16 * LD + kInt4BlockCols * u + 8 * quarter, LD,
-                                                                s_sum[turn] + u * PER_BLOCK * TOKENS + 4 * quarter);
+                int4_block<2, TILES, PER_BLOCK, BLOCKS, TOKENS>(acc, w[u], u, scale_of, zero_of, true, s_x[turn] + x_at + kInt4BlockCols * u, LD,
+                                                                s_sum[turn] + u * PER_BLOCK * TOKENS + sum_at);
             }
+        };
+        const int span = a.blocks_per_group > 1 ? AT_ONCE * a.blocks_per_group : AT_ONCE / PER_BLOCK;  // blocks whose scales lie in LDS
+        int turn = 0;
+        for (int s0 = 0; s0 < a.blocks; s0 += span) {
+            const int g_from = a.blocks_per_group > 1 ? s0 / a.blocks_per_group : s0 * PER_BLOCK, s1 = min(a.blocks, s0 + span);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();  // the wavefront has read those before
+            fill(g_from);
+            for (int b = s0; b < s1; b += BLOCKS, turn ^= 1) one_step(b, g_from, turn);
         }
 #pragma unroll
         for (int t = 0; t < TILES; t++) {

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(64 * kMmWaves, TILES == 8 ? 1 : 2) void k_int4_mm(c
         auto load_x = [&](int blk) {
 #pragma unroll
             for (int t = 0; t < TILES; t++)
-                if (t < tiles) x_next[t] = int4_x(x_row[t], kInt4BlockCols * blk + 8 * piece, a.cols);
+                if (t < tiles) x_next[t] = int4_x(x_row[t], kInt4BlockCols * blk + 8 * piece, a.cols, kInt4BlockCols * (blk + 1) <= a.cols);
         };
         auto load_w = [&](int blk) {
 #pragma unroll
