@@ -29,6 +29,10 @@ struct Int4Args {
     int split;                     // k_int4_split: wavefronts that share a tile of rows along the columns
 };
 
+// A value that is to be made here and not further down, where the compiler would like to make it beside others: sums that wait to be
+// scaled hold registers.
+__device__ __forceinline__ void int4_now(f32x4 &v) { asm volatile("" : "+v"(v)); }
+
 // One matrix as a wavefront reads it.  Its pointers may come out of an array in memory, so they are given their address space by
 // hand: through a generic pointer every load would also count as LDS traffic and be waited for together with it.
 using gp_bytes = const __attribute__((address_space(1))) uint8_t *;
@@ -146,9 +150,9 @@ __device__ __forceinline__ void int4_store(const Int4Args &a, size_t out_row, fl
 }
 
 // qmoe_int4_mm_*.hip
-qmoe_status launch_int4_mm_plain(const Int4Args &a, int cus, hipStream_t s);
-qmoe_status launch_int4_mm_zeros(const Int4Args &a, int cus, hipStream_t s);
-qmoe_status launch_int4_mm_gated(const Int4Args &a, int cus, hipStream_t s);
-qmoe_status launch_int4_mm_gated_zeros(const Int4Args &a, int cus, hipStream_t s);
+qmoe_status launch_int4_mm_plain(const Int4Args &a, int grid, hipStream_t s);
+qmoe_status launch_int4_mm_zeros(const Int4Args &a, int grid, hipStream_t s);
+qmoe_status launch_int4_mm_gated(const Int4Args &a, int grid, hipStream_t s);
+qmoe_status launch_int4_mm_gated_zeros(const Int4Args &a, int grid, hipStream_t s);
 
 }  // namespace qmoe

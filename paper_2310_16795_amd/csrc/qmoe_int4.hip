@@ -450,7 +450,7 @@ qmoe_status launch_few(Int4Args a, int tiles, long long items, int cus, hipStrea
 {
     const bool gated = int4_is_gated(a.activation);
     const long long row_tiles = (a.rows + 15) / 16, tile_units = items * ((a.rows + (gated ? 63 : 127)) / (gated ? 64 : 128));
-    if (tile_units < 2LL * cus) {
+    if (tile_units < 2LL * cus || a.cols < 8) {
         a.split = 1;
         while (a.split < kInt4MaxSplit && a.split < a.blocks && items * row_tiles * a.split < 16LL * cus) a.split *= 2;
         const int grid = (int)std::min<long long>(items * row_tiles, 32LL * cus);
@@ -462,11 +462,16 @@ qmoe_status launch_few(Int4Args a, int tiles, long long items, int cus, hipStrea
     return launch_tile_variant<4>(a, grid, s);
 }
 
-// zeros: a matrix has zero points (descriptors in device memory: may have)
-qmoe_status launch_mm_kernel(const Int4Args &a, bool zeros, int cus, hipStream_t s)
+// Tiles of 64 tokens, `items` of them about; zeros: a matrix has zero points (descriptors in device memory: may have).  The kernel for
+// many tokens where its blocks of rows are enough for the compute units, else the one with blocks half as high.
+qmoe_status launch_many(const Int4Args &a, bool zeros, long long items, int cus, hipStream_t s)
 {
-    if (int4_is_gated(a.activation)) return zeros ? launch_int4_mm_gated_zeros(a, cus, s) : launch_int4_mm_gated(a, cus, s);
-    return zeros ? launch_int4_mm_zeros(a, cus, s) : launch_int4_mm_plain(a, cus, s);
+    const bool gated = int4_is_gated(a.activation);
+    const long long units = items * ((a.rows + (gated ? 127 : 255)) / (gated ? 128 : 256));
+    if (units < cus || a.cols < 8) return launch_few(a, 4, items, cus, s);
+    const int grid = (int)std::min<long long>(units, 64LL * cus);
+    if (gated) return zeros ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
+    return zeros ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
 }
 
 }  // namespace
@@ -501,7 +506,7 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W, const uint16_t *x_bf16, 
     a.out_f32 = y_type == QMOE_F32;
     a.activation = activation;
     fill_shape(&a, rows, W->cols, W->group);
-    if (batch > 64) return launch_mm_kernel(a, a.zero != nullptr, di.cus, static_cast<hipStream_t>(stream));
+    if (batch > 64) return launch_many(a, a.zero != nullptr, (batch + 63) / 64, di.cus, static_cast<hipStream_t>(stream));
     const int tiles = (batch + 15) / 16, at_once = tiles <= 2 ? tiles : 4;
     return launch_few(a, tiles, (tiles + at_once - 1) / at_once, di.cus, static_cast<hipStream_t>(stream));
 }
@@ -545,7 +550,7 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
         a.items = g.many;
         a.n_items_dev = g.n_many;
         a.max_items = n_tokens / kInt4FewTokens;  // (each has more than that, or stands beside a whole tile)
-        return launch_few(a, 4, a.max_items, di.cus, s);
+        return launch_many(a, true, a.max_items, di.cus, s);
     };
     if ((st = product()) != QMOE_OK) return st;
     a.mats = wo;

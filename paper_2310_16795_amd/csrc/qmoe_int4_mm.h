@@ -6,138 +6,180 @@
 namespace qmoe {
 namespace {
 
-// A workgroup of four wavefronts multiplies 64 * ROWS rows (gated: 32 * ROWS of each projection) with 16 * TILES tokens, 128 columns
-// at a time.  The activations of a step go through LDS, which all four read; the weights of a row are one
-// wavefront's alone and go from memory into its registers, 16 bytes a lane, and there become the operands of the matrix
-// instruction (int4_plus16): decoded once for all the tokens of the tile.
-// With PER_BLOCK groups of 128 / PER_BLOCK columns, a group's sum starts at -(16 + z) * sum of x (the sums of x are formed by
-// those who stage it) and is scaled into the result in fp32.
-constexpr int kMmWaves = 4;
-constexpr int kXRow = kInt4BlockCols + 8;  // bf16 values from a token's row in LDS to the next: 16 lanes' 16-byte reads meet no bank twice
+// A workgroup of four wavefronts multiplies 256 rows (gated: 128 of each projection) with 64 tokens, 128 columns a step: four tiles of 16 rows
+// a wavefront, 64 matrix instructions a step.
+// The activations go through LDS in two turns and are read by all four; a wavefront's weights are its alone: loaded 64 bytes a row,
+// brought to their lanes by ds_bpermute and decoded (int4_plus16) 32 columns at a time, right before the 16 matrix instructions that use
+// them, so that decoding one tile runs beside multiplying the one before and few registers hold operands.  Two wavefronts a SIMD: the
+// sums (64 registers) are scaled into the result (64) in fp32, which accumulation registers could not take part in.
+// With PER_BLOCK groups of 128 / PER_BLOCK columns, a group's sum starts at -(16 + z) * sum of x (formed by those who stage x).
+// Scales and zero points of AT_ONCE groups lie in LDS, a wavefront's own.
+constexpr int kMmRows = 4, kMmTiles = 4, kMmAtOnce = 32;
 
-template <int ROWS, int TILES, bool GATED, bool ZEROS, int PER_BLOCK>
-__global__ __launch_bounds__(64 * kMmWaves, TILES == 8 ? 1 : 2) void k_int4_mm(const Int4Args a)
+template <bool GATED, bool ZEROS, int PER_BLOCK>
+__global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
 {
-    constexpr int TOKENS = 16 * TILES, OUT_TILES = GATED ? ROWS / 2 : ROWS;
-    __shared__ __align__(16) uint16_t s_x[2][TOKENS * kXRow];
-    __shared__ __align__(16) float s_sum[2][PER_BLOCK][TOKENS];
+    constexpr int TOKENS = 16 * kMmTiles, OUT_TILES = GATED ? kMmRows / 2 : kMmRows, LD = kInt4BlockCols + 8;
+    constexpr int LD_SCALE = kMmAtOnce + 8, LD_ZERO = kMmAtOnce + 8;
+    __shared__ __align__(16) uint16_t s_x[2][TOKENS * LD];
+    __shared__ __align__(16) float s_sum[2][PER_BLOCK * TOKENS];
+    __shared__ __align__(16) uint16_t s_scale[4][16 * kMmRows * LD_SCALE];
+    __shared__ __align__(16) uint8_t s_zero[4][ZEROS ? 16 * kMmRows * LD_ZERO : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int n16 = lane & 15, quarter = lane >> 4;
-    const int piece = threadIdx.x & 15, stager = threadIdx.x >> 4;  // stages 8 columns of tokens stager + 16 i
-    const int row_blocks = (a.rows + 16 * OUT_TILES * kMmWaves - 1) / (16 * OUT_TILES * kMmWaves);
+    const int n16 = lane & 15, quarter = lane >> 4, from_lane = 4 * (4 * n16 + quarter);
+    const int piece = threadIdx.x & 15, stager = threadIdx.x >> 4;  // stages 8 columns of tokens stager + 16 t
+    const int row_blocks = (a.rows + 64 * OUT_TILES - 1) / (64 * OUT_TILES);
     const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
     const long long total = (long long)n_items * row_blocks;
     const size_t row_bytes = (size_t)64 * a.blocks;
     for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
-        const int item = (int)(unit / row_blocks), rb = (int)(unit - (long long)item * row_blocks);
+        // Workgroups go to the eight XCDs in turn: an XCD's units follow each other, and those of a whole matrix go by eight tiles of
+        // tokens, so that what it holds at a time shares rows and activations in its L2.
+        long long at = unit;
+        int item, rb;
+        if (a.items) {
+            item = (int)(at / row_blocks), rb = (int)(at - (long long)item * row_blocks);
+        } else {
+            const long long whole = total / 8 * 8;
+            if (at < whole) at = (at & 7) * (whole / 8) + (at >> 3);
+            const int tiles8 = n_items / 8;  // whole groups of eight tiles
+            const int group = (int)(at / (8LL * row_blocks)), in = (int)(at - group * 8LL * row_blocks);
+            const int wide = group < tiles8 ? 8 : n_items - 8 * tiles8;
+            rb = in / wide, item = 8 * group + in % wide;
+        }
         int expert = 0, slot0 = item * TOKENS, ntok = min(TOKENS, a.batch - slot0);
         if (a.items) {
             const Item it = a.items[item];
             expert = it.expert, slot0 = it.slot0, ntok = min(it.ntok, TOKENS);
         }
-        const int tiles = (ntok + 15) / 16;
         const Int4Matrix m = int4_matrix(a, expert);
-        const int tile0 = (rb * kMmWaves + wave) * OUT_TILES;
-        const uint8_t *w_row[ROWS];
-        size_t meta[ROWS];
+        const int first = 16 * OUT_TILES * (4 * rb + wave);  // row of this wavefront
+        // the matrix's row that a tile's row is
+        auto row_of = [&](int r, int in_tile) {
+            return (size_t)(min(first + 16 * (r % OUT_TILES) + in_tile, a.rows - 1) + (r / OUT_TILES) * a.rows);
+        };
+        const uint8_t *w_row[kMmRows];
 #pragma unroll
-        for (int r = 0; r < ROWS; r++) {
-            const int row = min(16 * (tile0 + r % OUT_TILES) + n16, a.rows - 1) + (r / OUT_TILES) * a.rows;
-            w_row[r] = m.weights + (size_t)row * row_bytes + 16 * quarter;
-            meta[r] = (size_t)row * a.groups;
-        }
-        const uint16_t *x_row[TILES];
+        for (int r = 0; r < kMmRows; r++) w_row[r] = m.weights + row_of(r, lane >> 2) * row_bytes + 16 * (lane & 3);
+        const uint16_t *x_row[kMmTiles];
 #pragma unroll
-        for (int t = 0; t < TILES; t++) {
+        for (int t = 0; t < kMmTiles; t++) {
             const int slot = slot0 + min(16 * t + stager, ntok - 1);
             x_row[t] = a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
         }
-        u32x4 x_next[TILES], w_next[ROWS];
-        uint16_t scale_next[ROWS][PER_BLOCK];
-        uint8_t zero_next[ROWS][PER_BLOCK];
-        auto load_x = [&](int blk) {
+        u32x4 x_next[kMmTiles], w_next[kMmRows];
+        auto load = [&](int blk) {
 #pragma unroll
-            for (int t = 0; t < TILES; t++)
-                if (t < tiles) x_next[t] = int4_x(x_row[t], kInt4BlockCols * blk + 8 * piece, a.cols, kInt4BlockCols * (blk + 1) <= a.cols);
+            for (int t = 0; t < kMmTiles; t++) x_next[t] = int4_x_load(x_row[t], kInt4BlockCols * blk + 8 * piece, a.cols);
+#pragma unroll
+            for (int r = 0; r < kMmRows; r++) w_next[r] = *(gp_u32x4)(w_row[r] + (size_t)64 * blk);
         };
-        auto load_w = [&](int blk) {
+        auto stage = [&](int blk, int buf) {
+            if (kInt4BlockCols * (blk + 1) > a.cols) {
 #pragma unroll
-            for (int r = 0; r < ROWS; r++) {
-                w_next[r] = *(gp_u32x4)(w_row[r] + (size_t)64 * blk);
-#pragma unroll
-                for (int g = 0; g < PER_BLOCK; g++) {
-                    const int of = PER_BLOCK > 1 ? blk * PER_BLOCK + g : (int)((uint32_t)blk / (uint32_t)a.blocks_per_group);
-                    const size_t at = meta[r] + min(of, a.groups - 1);
-                    scale_next[r][g] = m.scale[at];
-                    if constexpr (ZEROS) zero_next[r][g] = m.zero ? m.zero[at] : 8;
-                }
+                for (int t = 0; t < kMmTiles; t++) x_next[t] = int4_x_end(x_next[t], kInt4BlockCols * blk + 8 * piece, a.cols);
             }
-        };
-        auto stage_x = [&](int buf) {
 #pragma unroll
-            for (int t = 0; t < TILES; t++) {
-                if (t >= tiles) break;
+            for (int t = 0; t < kMmTiles; t++) {
                 const int token = 16 * t + stager;
-                *reinterpret_cast<u32x4 *>(&s_x[buf][token * kXRow + 8 * piece]) = x_next[t];
+                *reinterpret_cast<u32x4 *>(&s_x[buf][token * LD + 8 * piece]) = x_next[t];
                 const float s = int4_group_sum<PER_BLOCK>(x_next[t]);
-                if ((piece + 1) % (16 / PER_BLOCK) == 0) s_sum[buf][piece / (16 / PER_BLOCK)][token] = ZEROS ? s : -24.0f * s;
+                if ((piece + 1) % (16 / PER_BLOCK) == 0) s_sum[buf][(piece * PER_BLOCK / 16) * TOKENS + token] = ZEROS ? s : -24.0f * s;
             }
         };
-        f32x4 acc[ROWS][TILES];
+        // groups g0 .. g0 + kMmAtOnce - 1 of the wavefront's 64 rows: four lanes a row, eight groups a lane
+        auto fill = [&](int g0) {
 #pragma unroll
-        for (int r = 0; r < ROWS; r++)
-#pragma unroll
-            for (int t = 0; t < TILES; t++) acc[r][t] = (f32x4){0, 0, 0, 0};
-        load_x(0);
-        load_w(0);
-        __syncthreads();  // the unit before has read its last step
-        stage_x(0);
-        __syncthreads();
-        for (int blk = 0; blk < a.blocks; blk++) {
-            const int buf = blk & 1;
-            bf16x8 wf[ROWS][4];
-            float scale[ROWS][PER_BLOCK], zero[ROWS][PER_BLOCK];
-#pragma unroll
-            for (int r = 0; r < ROWS; r++) {
-#pragma unroll
-                for (int s = 0; s < 4; s++) wf[r][s] = int4_plus16(w_next[r][s]);
-#pragma unroll
-                for (int g = 0; g < PER_BLOCK; g++) {
-                    scale[r][g] = half_bits_to_float(scale_next[r][g]);
-                    if constexpr (ZEROS) zero[r][g] = -16.0f - (float)zero_next[r][g];
+            for (int r = 0; r < kMmRows; r++) {
+                const int in_tile = lane >> 2, at8 = 8 * (lane & 3);
+                const size_t row = row_of(r, in_tile) * a.groups;
+                uint16_t *to = &s_scale[wave][(16 * r + in_tile) * LD_SCALE + at8];
+                uint8_t *to_zero = &s_zero[wave][ZEROS ? (16 * r + in_tile) * LD_ZERO + at8 : 0];
+                if (g0 + at8 + 8 <= a.groups) {
+                    uint32_t v[4], z[2] = {0x08080808u, 0x08080808u};
+                    int4_load_packed<16>(v, m.scale + (row + g0 + at8));
+                    if (ZEROS && m.zero) int4_load_packed<8>(z, m.zero + (row + g0 + at8));
+                    *reinterpret_cast<u32x4 *>(to) = (u32x4){v[0], v[1], v[2], v[3]};
+                    if constexpr (ZEROS) *reinterpret_cast<uint2 *>(to_zero) = make_uint2(z[0], z[1]);
+                } else {
+                    for (int i = 0; i < 8; i++) {  // 0 behind the last group: its columns are none, but what lies there could be infinite
+                        const bool is = g0 + at8 + i < a.groups;
+                        to[i] = is ? m.scale[row + g0 + at8 + i] : 0;
+                        if constexpr (ZEROS) to_zero[i] = is && m.zero ? m.zero[row + g0 + at8 + i] : 8;
+                    }
                 }
             }
-            if (blk + 1 < a.blocks) {
-                load_x(blk + 1);
-                load_w(blk + 1);
-            }
+        };
+        f32x4 acc[kMmRows][kMmTiles];
 #pragma unroll
-            for (int t = 0; t < TILES; t++) {
-                if (t >= tiles) break;
+        for (int r = 0; r < kMmRows; r++)
 #pragma unroll
-                for (int g = 0; g < PER_BLOCK; g++) {
-                    const f32x4 xs = *reinterpret_cast<const f32x4 *>(&s_sum[buf][g][16 * t + 4 * quarter]);
-                    f32x4 sum[ROWS];
+            for (int t = 0; t < kMmTiles; t++) acc[r][t] = (f32x4){0, 0, 0, 0};
+        load(0);
+        __syncthreads();  // the unit before has read its last step
+        stage(0, 0);
+        __syncthreads();
+        const int x_at = n16 * LD + 8 * quarter;
+        const int span = a.blocks_per_group > 1 ? kMmAtOnce * a.blocks_per_group : kMmAtOnce / PER_BLOCK;  // blocks whose scales lie in LDS
+        for (int s0 = 0; s0 < a.blocks; s0 += span) {
+            const int g_from = a.blocks_per_group > 1 ? s0 / a.blocks_per_group : s0 * PER_BLOCK, s1 = min(a.blocks, s0 + span);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();  // the wavefront has read those before
+            fill(g_from);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            for (int blk = s0; blk < s1; blk++) {
+                const int buf = blk & 1;
+                uint32_t w[kMmRows][4];
 #pragma unroll
-                    for (int r = 0; r < ROWS; r++) sum[r] = ZEROS ? xs * zero[r][g] : xs;
+                for (int r = 0; r < kMmRows; r++)
 #pragma unroll
-                    for (int s = g * 4 / PER_BLOCK; s < (g + 1) * 4 / PER_BLOCK; s++) {
-                        const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(&s_x[buf][(16 * t + n16) * kXRow + 32 * s + 8 * quarter]);
+                    for (int s = 0; s < 4; s++) w[r][s] = (uint32_t)__builtin_amdgcn_ds_bpermute(from_lane, (int)w_next[r][s]);
+                load(min(blk + 1, a.blocks - 1));
+                const int g_at = (a.blocks_per_group > 1 ? blk / a.blocks_per_group : blk * PER_BLOCK) - g_from;
+                f32x4 sum[kMmRows][kMmTiles];
 #pragma unroll
-                        for (int r = 0; r < ROWS; r++) sum[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, wf[r][s], sum[r], 0, 0, 0);
+                for (int s = 0; s < 4; s++) {
+                    const int g = s * PER_BLOCK / 4;
+                    __builtin_amdgcn_sched_barrier(0);  // (operands of several turns at once would not fit the registers)
+                    bf16x8 xf[kMmTiles];
+#pragma unroll
+                    for (int t = 0; t < kMmTiles; t++) xf[t] = *reinterpret_cast<const bf16x8 *>(&s_x[buf][x_at + 16 * t * LD + 32 * s]);
+                    if (s * PER_BLOCK % 4 == 0) {
+#pragma unroll
+                        for (int t = 0; t < kMmTiles; t++) {
+                            const f32x4 xs = *reinterpret_cast<const f32x4 *>(&s_sum[buf][g * TOKENS + 16 * t + 4 * quarter]);
+#pragma unroll
+                            for (int r = 0; r < kMmRows; r++) {
+                                if constexpr (ZEROS) sum[r][t] = xs * (-16.0f - (float)s_zero[wave][(16 * r + n16) * LD_ZERO + g_at + g]);
+                                else sum[r][t] = xs;
+                            }
+                        }
                     }
 #pragma unroll
-                    for (int r = 0; r < ROWS; r++)
+                    for (int r = 0; r < kMmRows; r++) {
+                        const bf16x8 wf = int4_plus16(w[r][s]);
 #pragma unroll
-                        for (int i = 0; i < 4; i++) acc[r][t][i] = fmaf(scale[r][g], sum[r][i], acc[r][t][i]);
+                        for (int t = 0; t < kMmTiles; t++) sum[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[t], wf, sum[r][t], 0, 0, 0);
+                    }
+                    if ((s + 1) * PER_BLOCK % 4) continue;
+#pragma unroll
+                    for (int r = 0; r < kMmRows; r++) {
+                        const float scale = half_bits_to_float(s_scale[wave][(16 * r + n16) * LD_SCALE + g_at + g]);
+#pragma unroll
+                        for (int t = 0; t < kMmTiles; t++)
+#pragma unroll
+                            for (int i = 0; i < 4; i++) acc[r][t][i] = fmaf(scale, sum[r][t][i], acc[r][t][i]);
+#pragma unroll
+                        for (int t = 0; t < kMmTiles; t++) int4_now(acc[r][t]);
+                    }
                 }
+                if (blk + 1 < a.blocks) stage(blk + 1, buf ^ 1);
+                __syncthreads();
             }
-            if (blk + 1 < a.blocks) stage_x(buf ^ 1);
-            __syncthreads();
         }
 #pragma unroll
-        for (int t = 0; t < TILES; t++) {
-            if (t >= tiles) break;
+        for (int t = 0; t < kMmTiles; t++) {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const int in_tile = 16 * t + 4 * quarter + i;
@@ -146,7 +188,7 @@ __global__ __launch_bounds__(64 * kMmWaves, TILES == 8 ? 1 : 2) void k_int4_mm(c
                 const float gate = a.gate ? a.gate[token] : 1.0f;
 #pragma unroll
                 for (int r = 0; r < OUT_TILES; r++) {
-                    const int row = 16 * (tile0 + r) + n16;
+                    const int row = first + 16 * r + n16;
                     if (row >= a.rows) continue;
                     float v = acc[r][t][i];
                     if constexpr (GATED) v = int4_gated(v, acc[r + OUT_TILES][t][i], a.activation);
@@ -157,28 +199,15 @@ __global__ __launch_bounds__(64 * kMmWaves, TILES == 8 ? 1 : 2) void k_int4_mm(c
     }
 }
 
-template <int ROWS, int TILES, bool GATED, bool ZEROS>
-qmoe_status launch_shape(const Int4Args &a, long long items, int cus, hipStream_t s)
+template <bool GATED, bool ZEROS>
+qmoe_status launch_mm(const Int4Args &a, int grid, hipStream_t s)
 {
-    const int block_rows = 16 * (GATED ? ROWS / 2 : ROWS) * kMmWaves;
-    const int grid = (int)std::min<long long>(items * ((a.rows + block_rows - 1) / block_rows), 16LL * cus);
-    const dim3 g(grid), b(64 * kMmWaves);
-    if (a.per_block == 1) hipLaunchKernelGGL((k_int4_mm<ROWS, TILES, GATED, ZEROS, 1>), g, b, 0, s, a);
-    else if (a.per_block == 2) hipLaunchKernelGGL((k_int4_mm<ROWS, TILES, GATED, ZEROS, 2>), g, b, 0, s, a);
-    else hipLaunchKernelGGL((k_int4_mm<ROWS, TILES, GATED, ZEROS, 4>), g, b, 0, s, a);
+    const dim3 g(grid), b(256);
+    if (a.per_block == 1) hipLaunchKernelGGL((k_int4_mm<GATED, ZEROS, 1>), g, b, 0, s, a);
+    else if (a.per_block == 2) hipLaunchKernelGGL((k_int4_mm<GATED, ZEROS, 2>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((k_int4_mm<GATED, ZEROS, 4>), g, b, 0, s, a);
     QMOE_HIP_TRY(hipGetLastError());
     return QMOE_OK;
-}
-
-template <bool GATED, bool ZEROS>
-qmoe_status launch_mm(const Int4Args &a, int cus, hipStream_t s)
-{
-    if (a.items) return launch_shape<2, 4, GATED, ZEROS>(a, a.max_items, cus, s);
-    const long long tiles128 = (a.batch + 127) / 128, blocks = (a.rows + (GATED ? 127 : 255)) / (GATED ? 128 : 256);
-    if (tiles128 * blocks >= cus) return launch_shape<4, 8, GATED, ZEROS>(a, tiles128, cus, s);
-    const long long tiles64 = (a.batch + 63) / 64;
-    if (tiles64 * blocks >= cus) return launch_shape<4, 4, GATED, ZEROS>(a, tiles64, cus, s);
-    return launch_shape<2, 4, GATED, ZEROS>(a, tiles64, cus, s);
 }
 
 }  // namespace

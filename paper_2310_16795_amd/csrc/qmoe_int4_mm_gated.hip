@@ -3,6 +3,6 @@
 
 namespace qmoe {
 
-qmoe_status launch_int4_mm_gated(const Int4Args &a, int cus, hipStream_t s) { return launch_mm<true, false>(a, cus, s); }
+qmoe_status launch_int4_mm_gated(const Int4Args &a, int grid, hipStream_t s) { return launch_mm<true, false>(a, grid, s); }
 
 }  // namespace qmoe

@@ -3,6 +3,6 @@
 
 namespace qmoe {
 
-qmoe_status launch_int4_mm_zeros(const Int4Args &a, int cus, hipStream_t s) { return launch_mm<false, true>(a, cus, s); }
+qmoe_status launch_int4_mm_zeros(const Int4Args &a, int grid, hipStream_t s) { return launch_mm<false, true>(a, grid, s); }
 
 }  // namespace qmoe

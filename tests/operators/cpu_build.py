@@ -53,7 +53,7 @@ def build(into: str) -> str:
     with open(os.path.join(src, "operators_cpu.h"), "w") as f:
         f.write(MORE)
     plain, units = lanes_build.converted, lanes_build.UNITS
-    lanes_build.converted = lambda text: '#include "operators_cpu.h"\n' + re.sub(r'asm\("" : "\+[sv]"\(\w+\)\);', "", plain(text))
+    lanes_build.converted = lambda text: '#include "operators_cpu.h"\n' + re.sub(r'asm( volatile)?\("" : "\+[sv]"\(\w+\)\);', "", plain(text))
     lanes_build.UNITS = units + UNITS
     more, lanes_build.NO_MATRIX_CORES = lanes_build.NO_MATRIX_CORES, lanes_build.NO_MATRIX_CORES + ROUND
     try:
