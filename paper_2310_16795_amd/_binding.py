@@ -377,46 +377,60 @@ def qmoe_bf16_layer_forward(wi_ptrs, wo_ptrs, n_experts: int, d_model: int, d_ff
 
 # ------------------------------------------------------------------ around the layer
 
-def _type_of(t, what: str) -> int:
-    """QMOE_F32 or QMOE_BF16 of a tensor (16-bit integers stand for bf16 bits)."""
-    import torch
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype in (torch.bfloat16, torch.int16) or t.dtype == getattr(torch, "uint16", None):
-        return BF16
-    raise ValueError(f"{what} must be float32 or bfloat16")
+_TYPES: dict = {}  # torch dtype -> QMOE_F32 / QMOE_BF16 (16-bit integers stand for bf16 bits)
 
 
-def _rows_ptr(t, what: str) -> int:
-    """Address of a device matrix whose rows are contiguous, any number of elements apart."""
+def _types() -> dict:
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.int16: BF16})
+        if hasattr(torch, "uint16"):
+            _TYPES[torch.uint16] = BF16
+    return _TYPES
+
+
+def _matrix(t, rows: int, cols: int, what: str):
+    """(address, QMOE_F32 or QMOE_BF16, elements from row to row) of a device matrix of contiguous rows."""
+    if t.shape != (rows, cols):
+        raise ValueError(f"shape mismatch: {what} must be [{rows}, {cols}]")
     if not t.is_cuda:
         raise ValueError("device tensor expected")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    kind = (_TYPES or _types()).get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{what} must be float32 or bfloat16")
+    if t.is_contiguous():
+        return t.data_ptr(), kind, cols
+    ld, unit = t.stride()
+    if (cols > 1 and unit != 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{what} must be a matrix of contiguous rows")
-    return t.data_ptr()
+    return t.data_ptr(), kind, ld if rows > 1 else cols
 
 
-def _row_stride(t) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+def _bf16_matrix(t, rows: int, cols: int, what: str):
+    p, kind, ld = _matrix(t, rows, cols, what)
+    if kind != BF16:
+        raise ValueError(f"{what} must be bfloat16")
+    return p, ld
 
 
 def _vector(t, n: int, what: str) -> int:
     """Address of a contiguous device float32 array of n values (None -> NULL)."""
-    import torch
     if t is None:
         return 0
-    if t.dtype != torch.float32 or t.numel() != n:
+    if (_TYPES or _types()).get(t.dtype) != F32 or t.numel() != n:
         raise ValueError(f"{what} must be float32 with {n} values")
     return _dev_ptr(t)
 
 
 def _norm_ptr(n, d: int, what: str):
-    """n: qmoe_norm, an object with one in .desc and its width in .d (device.DeviceNorm), or None."""
+    """n: a qmoe_norm, an object with one in .desc and its width in .d (device.DeviceNorm), or None."""
     if n is None:
         return None
-    if getattr(n, "d", d) not in (None, d):
+    if isinstance(n, qmoe_norm):
+        return byref(n)
+    if n.d is not None and n.d != d:
         raise ValueError(f"{what} is a norm of {n.d} values, not {d}")
-    return byref(getattr(n, "desc", n))
+    return n.ref
 
 
 def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, post=None, alpha: float = 1.0, channel_scale=None,
@@ -424,34 +438,31 @@ def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, pos
     """h, h_out: device [n, d] float32 or bfloat16 (h_out may be h); y: [n * k, d] float32 or bfloat16; x: [n * copies, d] bfloat16;
     gate: float32, n * k values; channel_scale: float32 [d]; post, pre: device.DeviceNorm."""
     n, d = h.shape
-    if y is not None and tuple(y.shape) != (n * k, d) or h_out is not None and (h_out.shape != h.shape or h_out.dtype != h.dtype) or \
-            x is not None and tuple(x.shape) != (n * copies, d):
-        raise ValueError("shape mismatch")
-    if x is not None and _type_of(x, "x") != BF16:
-        raise ValueError("x must be bfloat16")
-    _check(lib().qmoe_residual_norm(
-        _rows_ptr(h, "h"), _type_of(h, "h"), _row_stride(h), 0 if y is None else _rows_ptr(y, "y"), 0 if y is None else _type_of(y, "y"),
-        0 if y is None else _row_stride(y), k, _vector(gate, n * k, "gate"), _norm_ptr(post, d, "post"), alpha,
-        _vector(channel_scale, d, "channel_scale"), _norm_ptr(pre, d, "pre"), 0 if h_out is None else _rows_ptr(h_out, "h_out"),
-        0 if h_out is None else _row_stride(h_out), 0 if x is None else _rows_ptr(x, "x"), 0 if x is None else _row_stride(x),
-        copies, n, d, _stream_ptr(stream)), "qmoe_residual_norm")
+    hp, ht, hl = _matrix(h, n, d, "h")
+    yp, yt, yl = (0, 0, 0) if y is None else _matrix(y, n * k, d, "y")
+    op, ot, ol = (0, ht, 0) if h_out is None else _matrix(h_out, n, d, "h_out")
+    xp, xl = (0, 0) if x is None else _bf16_matrix(x, n * copies, d, "x")
+    if ot != ht:
+        raise ValueError("h_out must be of h's type")
+    _check(lib().qmoe_residual_norm(hp, ht, hl, yp, yt, yl, k, _vector(gate, n * k, "gate"), _norm_ptr(post, d, "post"), alpha,
+                                    _vector(channel_scale, d, "channel_scale"), _norm_ptr(pre, d, "pre"), op, ol, xp, xl, copies, n, d,
+                                    _stream_ptr(stream)), "qmoe_residual_norm")
 
 
 def qmoe_route(logits, expert_idx, gate, bias=None, token_mask=None, gates: int = GATES_ALL, stream=None) -> None:
     """logits: device [n, n_experts] float32 or bfloat16; expert_idx: int32 [n, k]; gate: float32 [n, k]; bias: float32
     [n_experts]; token_mask: one byte (or bool) a token, 0 = padding."""
-    import torch
     n, n_experts = logits.shape
-    k = expert_idx.shape[1]
-    if tuple(expert_idx.shape) != (n, k) or tuple(gate.shape) != (n, k):
+    lp, lt, ld = _matrix(logits, n, n_experts, "logits")
+    shape = expert_idx.shape
+    if len(shape) != 2 or shape[0] != n or gate.shape != shape:
         raise ValueError("shape mismatch")
-    if expert_idx.dtype != torch.int32 or gate.dtype != torch.float32:
-        raise ValueError("expert_idx must be int32, gate float32")
+    if expert_idx.element_size() != 4 or expert_idx.is_floating_point():
+        raise ValueError("expert_idx must be int32")
     if token_mask is not None and (token_mask.numel() != n or token_mask.element_size() != 1):
         raise ValueError("token_mask must hold a byte for every token")
-    _check(lib().qmoe_route(_rows_ptr(logits, "logits"), _type_of(logits, "logits"), _row_stride(logits),
-                            _vector(bias, n_experts, "bias"), _dev_ptr(token_mask), n, n_experts, k, gates, _dev_ptr(expert_idx),
-                            _dev_ptr(gate), _stream_ptr(stream)), "qmoe_route")
+    _check(lib().qmoe_route(lp, lt, ld, _vector(bias, n_experts, "bias"), _dev_ptr(token_mask), n, n_experts, shape[1], gates,
+                            _dev_ptr(expert_idx), _vector(gate, n * shape[1], "gate"), _stream_ptr(stream)), "qmoe_route")
 
 
 # ------------------------------------------------------------------ four-bit weights
@@ -496,28 +507,27 @@ def qmoe_int4_quantize_host(w: np.ndarray, group: int = 128, zero: bool = False)
 
 def qmoe_int4_matvec(W: qmoe_int4_matrix, x_bf16, y, activation: int = ACT_NONE, stream=None) -> None:
     """x_bf16: device bfloat16 [batch, cols]; y: device float32 or bfloat16 [batch, rows] (gated activations: rows / 2)."""
-    batch, cols = x_bf16.shape
-    if cols != W.cols or tuple(y.shape) != (batch, W.rows // 2 if activation >= ACT_SILU_GATED else W.rows):
-        raise ValueError("shape mismatch")
-    if _type_of(x_bf16, "x") != BF16:
-        raise ValueError("x must be bfloat16")
-    _check(lib().qmoe_int4_matvec(byref(W), _rows_ptr(x_bf16, "x"), _row_stride(x_bf16), batch, activation, _rows_ptr(y, "y"),
-                                  _type_of(y, "y"), _row_stride(y), _stream_ptr(stream)), "qmoe_int4_matvec")
+    batch, rows = x_bf16.shape[0], W.rows
+    xp, xl = _bf16_matrix(x_bf16, batch, W.cols, "x")
+    yp, yt, yl = _matrix(y, batch, rows // 2 if activation >= ACT_SILU_GATED else rows, "y")
+    _check(lib().qmoe_int4_matvec(byref(W), xp, xl, batch, activation, yp, yt, yl, _stream_ptr(stream)), "qmoe_int4_matvec")
 
 
 def qmoe_int4_layer_forward(wi_dev, wo_dev, group: int, activation: int, n_experts: int, d_model: int, d_ff: int, x_bf16, expert_idx,
                             gate, y, workspace, stream=None) -> None:
     """wi_dev / wo_dev: device byte tensors holding n_experts qmoe_int4_matrix structs; y: float32 or bfloat16."""
     n_tokens = x_bf16.shape[0]
-    if tuple(x_bf16.shape) != (n_tokens, d_model) or tuple(y.shape) != (n_tokens, d_model) or expert_idx.numel() != n_tokens:
-        raise ValueError("shape mismatch")
-    if _type_of(x_bf16, "x") != BF16 or expert_idx.element_size() != 4:
-        raise ValueError("x must be bfloat16, expert_idx int32")
-    if min(t.numel() * t.element_size() for t in (wi_dev, wo_dev)) < _INT4_BYTES * n_experts:
+    xp, xl = _bf16_matrix(x_bf16, n_tokens, d_model, "x")
+    yp, yt, yl = _matrix(y, n_tokens, d_model, "y")
+    if expert_idx.numel() != n_tokens or expert_idx.element_size() != 4:
+        raise ValueError("expert_idx must be int32, one for every token")
+    if xl != d_model or yl != d_model:
+        raise ValueError("contiguous tensor expected")
+    need = _INT4_BYTES * n_experts
+    if wi_dev.numel() * wi_dev.element_size() < need or wo_dev.numel() * wo_dev.element_size() < need:
         raise ValueError("expert descriptor arrays too small")
-    _check(lib().qmoe_int4_layer_forward(_dev_ptr(wi_dev), _dev_ptr(wo_dev), group, activation, n_experts, d_model, d_ff,
-                                         _dev_ptr(x_bf16), _dev_ptr(expert_idx), _vector(gate, n_tokens, "gate"), n_tokens,
-                                         _dev_ptr(y), _type_of(y, "y"), _dev_ptr(workspace),
+    _check(lib().qmoe_int4_layer_forward(_dev_ptr(wi_dev), _dev_ptr(wo_dev), group, activation, n_experts, d_model, d_ff, xp,
+                                         _dev_ptr(expert_idx), _vector(gate, n_tokens, "gate"), n_tokens, yp, yt, _dev_ptr(workspace),
                                          workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
            "qmoe_int4_layer_forward")
 

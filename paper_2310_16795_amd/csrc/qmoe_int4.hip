@@ -6,6 +6,7 @@ namespace {
 
 constexpr int kInt4MaxSplit = 8;
 constexpr int kInt4FewTokens = 16;  // of an expert: one tile of tokens; those with more get four
+constexpr int kInt4Direct = 4;      // layer calls of up to so many tokens do without the dispatch: an item a token
 constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens make no tiles but of 16
 
 // What both kernels here share.
@@ -115,7 +116,8 @@ __device__ __forceinline__ void int4_block(f32x4 (&acc)[SIDES][TILES], const u32
 
 // Results of 16 tokens (of the tile t) and the SIDES tiles of rows from row on; gated: the two are one's gate and product.
 template <int SIDES>
-__device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, const f32x4 (&v)[SIDES], int t, int row, int quarter, int slot0, int ntok)
+__device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, const f32x4 (&v)[SIDES], int t, int row, int quarter, int slot0, int ntok,
+                                             bool none = false)
 {
 #pragma unroll
     for (int k = 0; k < 4; k++) {
@@ -123,7 +125,7 @@ __device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, cons
         if (in_tile >= ntok) continue;
         const int token = a.perm ? a.perm[slot0 + in_tile] : slot0 + in_tile;
         const size_t out_row = a.out_by_slot ? slot0 + in_tile : token;
-        const float gate = a.gate ? a.gate[token] : 1.0f;
+        const float gate = none ? 0.0f : a.gate ? a.gate[token] : 1.0f;
         if (SIDES == 2 && gated) {
             if (row < a.rows) int4_store(a, out_row, gate, row, int4_gated(v[0][k], v[SIDES - 1][k], a.activation));
         } else {
@@ -138,12 +140,18 @@ __device__ __forceinline__ bool int4_gates(const Int4Args &a) { return a.activat
 
 struct Int4Unit {
     int expert, slot0, ntok;
+    bool none;  // a token without an expert: its results are 0
 };
 __device__ __forceinline__ Int4Unit int4_unit(const Int4Args &a, int item, int tokens)
 {
-    if (!a.items) return {0, item * tokens, min(tokens, a.batch - item * tokens)};
+    if (a.direct) {
+        const int e = a.direct[item];
+        const bool none = e < 0 || e >= a.n_experts;
+        return {none ? 0 : e, item, 1, none};
+    }
+    if (!a.items) return {0, item * tokens, min(tokens, a.batch - item * tokens), false};
     const Item it = a.items[item];
-    return {it.expert, it.slot0, min(it.ntok, tokens)};
+    return {it.expert, it.slot0, min(it.ntok, tokens), false};
 }
 __device__ __forceinline__ const uint16_t *int4_x_row(const Int4Args &a, int slot)
 {
@@ -165,12 +173,13 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
     f32x4 *joined = reinterpret_cast<f32x4 *>(smem);
     const bool gated = int4_gates(a);
     const int row_tiles = (a.rows + 15) / 16;
-    const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
+    const int n_items = a.direct ? a.max_items : a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
     const long long total = (long long)n_items * row_tiles;
-    const int b0 = (int)((long long)a.blocks * part / a.split), b1 = (int)((long long)a.blocks * (part + 1) / a.split);
+    const int b0 = (int)((long long)a.blocks * part / a.split), b_end = (int)((long long)a.blocks * (part + 1) / a.split);
     for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
         const int item = (int)(unit / row_tiles), tile = (int)(unit - (long long)item * row_tiles);
         const Int4Unit it = int4_unit(a, item, TOKENS);
+        const int b1 = it.none ? b0 : b_end;
         const Int4Matrix m = int4_matrix(a, it.expert);
         Int4Rows<SIDES, 1, PER_BLOCK> rows;
         int base[SIDES], behind[SIDES];
@@ -247,7 +256,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
                 v[g] = joined[(g * TILES + t) * 64 + lane];
                 for (int p = 1; p < a.split; p++) v[g] += joined[((p * SIDES + g) * TILES + t) * 64 + lane];
             }
-            int4_results<SIDES>(a, gated, v, t, 16 * tile + n16, quarter, it.slot0, it.ntok);
+            int4_results<SIDES>(a, gated, v, t, 16 * tile + n16, quarter, it.slot0, it.ntok, it.none);
         }
         __syncthreads();  // before the next unit's activations overwrite these
     }
@@ -450,7 +459,7 @@ qmoe_status launch_few(Int4Args a, int tiles, long long items, int cus, hipStrea
 {
     const bool gated = int4_is_gated(a.activation);
     const long long row_tiles = (a.rows + 15) / 16, tile_units = items * ((a.rows + (gated ? 63 : 127)) / (gated ? 64 : 128));
-    if (tile_units < 2LL * cus || a.cols < 8) {
+    if (tile_units < 2LL * cus || a.cols < 8 || a.direct) {
         a.split = 1;
         while (a.split < kInt4MaxSplit && a.split < a.blocks && items * row_tiles * a.split < 16LL * cus) a.split *= 2;
         const int grid = (int)std::min<long long>(items * row_tiles, 32LL * cus);
@@ -462,14 +471,15 @@ qmoe_status launch_few(Int4Args a, int tiles, long long items, int cus, hipStrea
     return launch_tile_variant<4>(a, grid, s);
 }
 
-// Tiles of 64 tokens, `items` of them about; zeros: a matrix has zero points (descriptors in device memory: may have).  The kernel for
-// many tokens where its blocks of rows are enough for the compute units, else the one with blocks half as high.
-qmoe_status launch_many(const Int4Args &a, bool zeros, long long items, int cus, hipStream_t s)
+// Tiles of 64 tokens, `items` of them about: the kernel for many tokens where its blocks of rows are enough for the compute units, else the
+// one with blocks half as high.
+qmoe_status launch_many(const Int4Args &a, long long items, int cus, hipStream_t s)
 {
     const bool gated = int4_is_gated(a.activation);
     const long long units = items * ((a.rows + (gated ? 127 : 255)) / (gated ? 128 : 256));
     if (units < cus || a.cols < 8) return launch_few(a, 4, items, cus, s);
     const int grid = (int)std::min<long long>(units, 64LL * cus);
+    const bool zeros = a.mats || a.zero;  // (descriptors in device memory: may have zero points)
     if (gated) return zeros ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
     return zeros ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
 }
@@ -506,7 +516,7 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W, const uint16_t *x_bf16, 
     a.out_f32 = y_type == QMOE_F32;
     a.activation = activation;
     fill_shape(&a, rows, W->cols, W->group);
-    if (batch > 64) return launch_many(a, a.zero != nullptr, (batch + 63) / 64, di.cus, static_cast<hipStream_t>(stream));
+    if (batch > 64) return launch_many(a, (batch + 63) / 64, di.cus, static_cast<hipStream_t>(stream));
     const int tiles = (batch + 15) / 16, at_once = tiles <= 2 ? tiles : 4;
     return launch_few(a, tiles, (tiles + at_once - 1) / at_once, di.cus, static_cast<hipStream_t>(stream));
 }
@@ -524,9 +534,13 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     hipStream_t s = static_cast<hipStream_t>(stream);
     DeviceInfo di;
     if ((st = gpu_info(&di)) != QMOE_OK) return st;
-    const bool crowded = n_tokens > kInt4AllFew;
-    GroupedTokens g;
-    if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, kInt4FewTokens,
+    const bool crowded = n_tokens > kInt4AllFew, direct = n_tokens <= kInt4Direct;
+    GroupedTokens g{};
+    if (direct) {
+        qmoe_ws_layout l;
+        if ((st = qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens, &l)) != QMOE_OK) return st;
+        g.hidden = reinterpret_cast<uint16_t *>(static_cast<unsigned char *>(workspace) + l.hidden);
+    } else if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, kInt4FewTokens,
                               crowded ? kInt4FewTokens + 1 : 0x7FFFFFFF, workspace, static_cast<float *>(y),
                               y_type == QMOE_F32 ? d_model : d_model / 2, s, &g)) != QMOE_OK)
         return st;
@@ -542,6 +556,11 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     a.activation = activation;
     fill_shape(&a, d_ff, d_model, group);
     auto product = [&]() {
+        if (direct) {
+            a.direct = expert_idx;
+            a.max_items = n_tokens;
+            return launch_few(a, 1, n_tokens, di.cus, s);
+        }
         a.items = g.few;
         a.n_items_dev = g.n_few;
         a.max_items = std::min(n_tokens, n_experts + n_tokens / kInt4FewTokens);
@@ -550,7 +569,7 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
         a.items = g.many;
         a.n_items_dev = g.n_many;
         a.max_items = n_tokens / kInt4FewTokens;  // (each has more than that, or stands beside a whole tile)
-        return launch_many(a, true, a.max_items, di.cus, s);
+        return launch_many(a, a.max_items, di.cus, s);
     };
     if ((st = product()) != QMOE_OK) return st;
     a.mats = wo;

@@ -78,12 +78,12 @@ __device__ __forceinline__ void store8(void *base, size_t at, int c, int d, cons
 // store, so that every value crosses memory once.  Workgroups either give each wavefront a row of its own (waves = 1; no
 // barrier) or are one row's.  The sums of a norm (of the values, then of the squares around the mean: no difference of
 // two large sums) go through DPP and, with several wavefronts, LDS; their order depends on the sizes alone.
-template <int HT, int YT, int PER>
-__global__ __launch_bounds__(1024) void k_residual_norm(const NormArgs a)
+template <int HT, int YT, int PER, bool ALONE>
+__global__ __launch_bounds__(ALONE ? 256 : 1024) void k_residual_norm(const NormArgs a)
 {
     __shared__ float sums[4][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool alone = a.waves == 1;
+    constexpr bool alone = ALONE;
     const long long row = alone ? (long long)blockIdx.x * (blockDim.x >> 6) + wave : blockIdx.x;
     if (row >= a.n_tokens) return;  // (a workgroup of one row leaves as one)
     const int me = alone ? lane : (int)threadIdx.x, step = 64 * a.waves * 8;
@@ -185,11 +185,14 @@ __global__ __launch_bounds__(1024) void k_residual_norm(const NormArgs a)
 }
 
 template <int HT, int YT>
-qmoe_status launch_norm(const NormArgs &a, int per, int grid, int threads, hipStream_t s)
+qmoe_status launch_norm(const NormArgs &a, int per, hipStream_t s)
 {
-    if (per == 1) hipLaunchKernelGGL((k_residual_norm<HT, YT, 1>), dim3(grid), dim3(threads), 0, s, a);
-    else if (per == 2) hipLaunchKernelGGL((k_residual_norm<HT, YT, 2>), dim3(grid), dim3(threads), 0, s, a);
-    else hipLaunchKernelGGL((k_residual_norm<HT, YT, 4>), dim3(grid), dim3(threads), 0, s, a);
+    const bool alone = a.waves == 1;
+    const dim3 grid(alone ? (a.n_tokens + 3) / 4 : a.n_tokens), threads(alone ? 256 : 64 * a.waves);
+    if (alone) hipLaunchKernelGGL((k_residual_norm<HT, YT, 1, true>), grid, threads, 0, s, a);
+    else if (per == 1) hipLaunchKernelGGL((k_residual_norm<HT, YT, 1, false>), grid, threads, 0, s, a);
+    else if (per == 2) hipLaunchKernelGGL((k_residual_norm<HT, YT, 2, false>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((k_residual_norm<HT, YT, 4, false>), grid, threads, 0, s, a);
     QMOE_HIP_TRY(hipGetLastError());
     return QMOE_OK;
 }
@@ -239,12 +242,10 @@ extern "C" qmoe_status qmoe_residual_norm(const void *h, int h_type, size_t ld_h
     const int eights = (d + 7) / 8;
     const int per = eights <= 1024 ? 1 : (eights <= 2048 ? 2 : 4);
     a.waves = (eights + 64 * per - 1) / (64 * per);
-    const int threads = a.waves == 1 ? 256 : 64 * a.waves;
-    const int grid = a.waves == 1 ? (n_tokens + 3) / 4 : n_tokens;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (h_type == QMOE_F32)
-        return y_type == QMOE_F32 ? launch_norm<QMOE_F32, QMOE_F32>(a, per, grid, threads, s)
-                                  : launch_norm<QMOE_F32, QMOE_BF16>(a, per, grid, threads, s);
-    return y_type == QMOE_F32 ? launch_norm<QMOE_BF16, QMOE_F32>(a, per, grid, threads, s)
-                              : launch_norm<QMOE_BF16, QMOE_BF16>(a, per, grid, threads, s);
+        return y_type == QMOE_F32 ? launch_norm<QMOE_F32, QMOE_F32>(a, per, s)
+                                  : launch_norm<QMOE_F32, QMOE_BF16>(a, per, s);
+    return y_type == QMOE_F32 ? launch_norm<QMOE_BF16, QMOE_F32>(a, per, s)
+                              : launch_norm<QMOE_BF16, QMOE_BF16>(a, per, s);
 }

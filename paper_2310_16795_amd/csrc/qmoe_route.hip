@@ -87,9 +87,39 @@ __device__ __forceinline__ void finish(const RouteArgs &a, int t, int l, int min
     }
 }
 
-// A token's keys lie in the registers of LANES lanes, expert l + LANES * i in lane l's register i: one pass over memory.
-// Each of the k rounds takes the largest key (a reduction over the lanes), of equal ones that of the lowest index (a
-// second one), and the lane that held it looks for its next best.
+// exp(v - top) for a sum: the hardware's exponential, off by |v - top| roundings or so, which where it counts is a few.  top is finite.
+__device__ __forceinline__ float share(float v, float top) { return __expf(v - top); }
+
+// Four consecutive logits from expert e on (n_experts a multiple of four, or elementwise).
+template <int TYPE>
+__device__ __forceinline__ void four_logits(float (&v)[4], const void *base, size_t row, int e, int n_experts, bool there)
+{
+    const bool whole = (n_experts & 3) == 0;
+#pragma unroll
+    for (int j = 0; j < 4; j++) v[j] = -INFINITY;
+    if (whole) {
+        if (there && e < n_experts) {
+            if constexpr (TYPE == QMOE_F32) {
+                const f32x4 q = *reinterpret_cast<const f32x4_by4 *>(static_cast<const float *>(base) + row + e);
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = q[j];
+            } else {
+                typedef uint32_t u32x2_by2 __attribute__((ext_vector_type(2), aligned(2)));
+                const u32x2_by2 q = *reinterpret_cast<const u32x2_by2 *>(static_cast<const uint16_t *>(base) + row + e);
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = __uint_as_float(j % 2 ? q[j / 2] & 0xFFFF0000u : q[j / 2] << 16);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            if (there && e + j < n_experts) v[j] = logit<TYPE>(base, row + e + j);
+    }
+}
+
+// A token's keys lie in the registers of LANES lanes, four neighbouring experts in a lane's four registers, then those 4 * LANES further: one
+// pass over memory.  Each of the k rounds takes the largest key (a reduction over the lanes), of equal ones that of the lowest
+// index (a second one), and the lane that held it looks for its next best.
 template <int TYPE, int LANES, int PER, bool BIAS>
 __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
 {
@@ -97,21 +127,25 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
     const int per_wave = 64 / LANES;
     const int t = (int)(blockIdx.x * 4 + wave) * per_wave + lane / LANES;
     const bool there = t < a.n_tokens && !(a.mask && a.mask[t] == 0);
+    auto expert = [&](int i) { return 4 * l + 4 * LANES * (i >> 2) + (i & 3); };
     float key[PER];
     float top = 0.0f, sum = 0.0f;
     {
         float v[PER];
 #pragma unroll
-        for (int i = 0; i < PER; i++) {
-            const int e = l + LANES * i;
-            v[i] = -INFINITY;
-            if (there && e < a.n_experts) v[i] = logit<TYPE>(a.logits, (size_t)t * a.ld + e);
+        for (int i = 0; i < PER; i += 4) {
+            float q[4];
+            four_logits<TYPE>(q, a.logits, (size_t)t * a.ld, expert(i), a.n_experts, there);
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[i + j] = q[j];
         }
         if constexpr (BIAS) {
 #pragma unroll
-            for (int i = 0; i < PER; i++) {
-                const int e = l + LANES * i;
-                key[i] = e < a.n_experts ? a.bias[e] : 0.0f;
+            for (int i = 0; i < PER; i += 4) {
+                float q[4];
+                four_logits<QMOE_F32>(q, a.bias, 0, expert(i), a.n_experts, true);
+#pragma unroll
+                for (int j = 0; j < 4; j++) key[i + j] = q[j];
             }
         }
 #pragma unroll
@@ -123,9 +157,9 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
             top = v[0];
 #pragma unroll
             for (int i = 1; i < PER; i++) top = fmaxf(top, v[i]);
-            top = lanes_max<LANES>(top);
+            top = fmaxf(lanes_max<LANES>(top), -FLT_MAX);
 #pragma unroll
-            for (int i = 0; i < PER; i++) sum += v[i] == -INFINITY ? 0.0f : expf(v[i] - top);
+            for (int i = 0; i < PER; i++) sum += share(v[i], top);
             sum = lanes_sum<LANES>(sum);
         }
     }
@@ -137,9 +171,10 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
     int mine = -1;
     for (int j = 0; j < a.k; j++) {
         const float m = lanes_max<LANES>(best);
-        const int e = lanes_min<LANES>(best == m ? l + LANES * best_i : 0x7FFFFFFF);
+        const int e = lanes_min<LANES>(best == m ? expert(best_i) : 0x7FFFFFFF);
         if (l == j) mine = m == -INFINITY ? -1 : e;
-        if (e == l + LANES * best_i) {  // one lane of the token's
+        if (j + 1 == a.k) break;
+        if (e == expert(best_i)) {  // one lane of the token's
             best = -INFINITY;
             const int gone = best_i;
 #pragma unroll

@@ -178,6 +178,7 @@ class DeviceNorm:
             raise ValueError("weight and bias must be float32 vectors of one width")
         self.weight, self.bias, self.d = weight, bias, given[0].numel() if given else None
         self.desc = B.qmoe_norm(self.KINDS[kind], eps, *(B._dev_ptr(t) or None for t in (weight, bias)))
+        self.ref = ctypes.byref(self.desc)
 
 
 def _int4_shapes(weights: torch.Tensor, scale: torch.Tensor, zero: "torch.Tensor | None", lead: tuple, cols: int, group: int):

@@ -13,6 +13,7 @@ UNITS = ["qmoe_norm.hip", "qmoe_route.hip", "qmoe_int4.hip", "qmoe_int4_mm_plain
 MORE = r"""#pragma once
 #include <hip/hip_runtime.h>
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, ...) lanes_mfma(a, b, c)
+#define __expf(x) expf(x)
 #define __builtin_amdgcn_ds_bpermute(from, v) lanes_bpermute(from, v)
 inline int lanes_bpermute(int from, int v) { return (int)(uint32_t)lanes::wave_values((uint32_t)v)[(from >> 2) & 63]; }
 template <class AB, class C> inline C lanes_mfma(AB a, AB b, C c)

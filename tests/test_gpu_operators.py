@@ -225,7 +225,7 @@ def test_int4_tokens_that_are_not_finite(gpu, batch):
 
 
 LAYERS = [  # experts, d_model, d_ff, tokens, group, zeros, activation, y, gate, routing
-    (1, 8, 8, 1, 32, False, "relu", "f32", False, "uniform"), (5, 264, 136, 1, 64, True, "silu", "bf16", True, "uniform"),
+    (1, 8, 8, 1, 32, False, "relu", "f32", False, "uniform"), (5, 72, 40, 4, 32, True, "silu", "bf16", True, "crowded"), (6, 200, 64, 5, 64, False, "gelu", "f32", True, "crowded"), (5, 264, 136, 1, 64, True, "silu", "bf16", True, "uniform"),
     (12, 256, 520, 40, 128, False, "relu", "f32", True, "uniform"), (7, 136, 264, 300, 32, True, "gelu", "bf16", False, "crowded"),
     (3, 512, 384, 700, 128, True, "silu", "f32", True, "crowded"), (64, 128, 256, 64, 64, False, "relu", "bf16", True, "uniform"),
     (4, 768, 640, 1500, 128, False, "relu", "bf16", True, "uniform"), (9, 72, 88, 33, 64, False, "relu", "f32", False, "none"),
@@ -247,15 +247,14 @@ def _check_layer(ex, x64, idx, gate, group, act, yt, y, ws, d_model, d_ff):
     """Each expert's hidden vectors as the workspace holds them, and the results from those (a value next to a rounding border
     may go either way in the first product; the second is held to what the first wrote)."""
     E, T = len(ex), idx.size
-    host = dev.read_workspace(ws, E, d_model, d_ff, T)
+    order = np.argsort(np.where((idx < 0) | (idx >= E), E, idx), kind="stable") if T > 4 else np.arange(T)  # slot -> token (few tokens: as they are)
     lay = q.qmoe_moe_layer_ws_layout(E, d_model, d_ff, T)
     hidden = plain.of_bits(ws.cpu().numpy()[lay.hidden:lay.hidden + 2 * T * d_ff].view(np.uint16)).reshape(T, d_ff)
     none = (idx < 0) | (idx >= E)
     assert not y[torch.from_numpy(none)].any()
     for e in range(E):
-        slots = np.arange(host["tok_off"][e], host["tok_off"][e + 1])
-        toks = host["perm"][slots]
-        assert np.array_equal(toks, np.flatnonzero(idx == e))
+        slots = np.flatnonzero(idx[order] == e)
+        toks = order[slots]
         if not toks.size:
             continue
         (vi, _, si, zi), (vo, _, so, zo) = ex[e]
@@ -272,7 +271,7 @@ def test_int4_layer(gpu, E, d_model, d_ff, T, group, zeros, act, yt, gated, rout
     ex, layer = _layer(gpu, rng, E, d_model, d_ff, group, zeros, act)
     idx = rng.integers(0, E, T).astype(np.int32)
     if routing == "crowded":
-        idx[: T // 2], idx[[3, T - 1]] = E - 1, (-1, E)
+        idx[: T // 2], idx[[min(3, T - 2), T - 1]] = E - 1, (-1, E)
     if routing == "none":
         idx[:] = -1
     gate = rng.random(T).astype(np.float32) if gated else None
