@@ -454,34 +454,54 @@ qmoe_status launch_tile_variant(const Int4Args &a, int grid, hipStream_t s)
     return QMOE_OK;
 }
 
-// tiles: tiles of 16 tokens of an item; items: how many the call has, about
+// What a call on one of the two kernels takes, us: rounds of workgroups (as many at a time as registers and LDS let a compute unit hold)
+// times a start of 4 and a time a block (split) or a step of two (tile) of one workgroup that is there alone, fitted to single matrices of
+// 1024 x 768, 4096 x 1024, 2080 x 6144 and 12288 x 2080, 1 to 1024 tokens, groups of 128.  Split / tile, measured: 2080 x 6144,
+// 1 token 7.6 / 28.6, 64 23 / 60, 192 45 / 62, 256 65 / 62; 4096 x 1024, 64 9.6 / 16, 128 17 / 17, 256 22 / 17; 12288 x 2080, 1 11 / 13.5,
+// 16 18.6 / 15.1, 64 71 / 28; 1024 x 768, 256 9.8 / 14, 512 17 / 14.
+double split_us(const Int4Args &a, int tiles, long long items, int cus)
+{
+    const double groups = (double)items * ((a.rows + 15) / 16), held = tiles == 1 ? 2.0 * cus : 1.0 * cus;
+    const int tokens = a.items ? 16 * tiles : std::min(a.batch, 16 * tiles);
+    const double block = (0.55 + 0.04 * tokens) * (tiles == 1 && groups > cus ? 1.6 : 1.0);
+    const double rounds = tiles == 1 ? std::max(1.0, groups / held) : std::ceil(groups / held);
+    return rounds * (4.0 + block * ((a.blocks + kInt4MaxSplit - 1) / kInt4MaxSplit));
+}
+double tile_us(const Int4Args &a, int tiles, long long units, int cus)
+{
+    const double held = tiles == 1 ? 4.0 * cus : 2.0 * cus, step = tiles == 1 ? 1.0 : tiles == 2 ? 1.4 : 2.4;
+    return std::max(1.0, (double)units / held) * (4.0 + step * ((a.blocks + 1) / 2));
+}
+
+// tiles: tiles of 16 tokens of an item; items: how many the call has, at most
 qmoe_status launch_few(Int4Args a, int tiles, long long items, int cus, hipStream_t s)
 {
     const bool gated = int4_is_gated(a.activation);
+    tiles = tiles <= 2 ? tiles : 4;
     const long long row_tiles = (a.rows + 15) / 16, tile_units = items * ((a.rows + (gated ? 63 : 127)) / (gated ? 64 : 128));
-    if (tile_units < 2LL * cus || a.cols < 8 || a.direct) {
+    if (a.direct || a.cols < 8 || split_us(a, tiles, items, cus) <= tile_us(a, tiles, tile_units, cus)) {
         a.split = 1;
         while (a.split < kInt4MaxSplit && a.split < a.blocks && items * row_tiles * a.split < 16LL * cus) a.split *= 2;
         const int grid = (int)std::min<long long>(items * row_tiles, 32LL * cus);
         return gated ? launch_split_sides<2>(a, tiles, grid, s) : launch_split_sides<1>(a, tiles, grid, s);
     }
     const int grid = (int)std::min<long long>(tile_units, 64LL * cus);
-    if (tiles <= 1) return launch_tile_variant<1>(a, grid, s);
-    if (tiles <= 2) return launch_tile_variant<2>(a, grid, s);
+    if (tiles == 1) return launch_tile_variant<1>(a, grid, s);
+    if (tiles == 2) return launch_tile_variant<2>(a, grid, s);
     return launch_tile_variant<4>(a, grid, s);
 }
 
-// Tiles of 64 tokens, `items` of them about: the kernel for many tokens where its blocks of rows are enough for the compute units, else the
-// one with blocks half as high.
-qmoe_status launch_many(const Int4Args &a, long long items, int cus, hipStream_t s)
+// More tokens of one matrix than a tile: the kernel for many where it fills the GPU one and a half times (12288 x 2080, 256 tokens 39 us, the
+// other way 38; 512 52 / 59; 1024 83 / 102).  In layer calls, where tiles are partly empty, it lost (16 experts of 1024 x 4096, 4001 tokens 213, the
+// other way 205; 64 of 1024 x 2048, 1000 tokens 122 / 99).
+qmoe_status launch_many(const Int4Args &a, int cus, hipStream_t s)
 {
     const bool gated = int4_is_gated(a.activation);
-    const long long units = items * ((a.rows + (gated ? 127 : 255)) / (gated ? 128 : 256));
-    if (units < cus || a.cols < 8) return launch_few(a, 4, items, cus, s);
+    const long long items = (a.batch + 63) / 64, units = items * ((a.rows + (gated ? 127 : 255)) / (gated ? 128 : 256));
+    if (2 * units < 3LL * cus || a.cols < 8) return launch_few(a, 4, items, cus, s);
     const int grid = (int)std::min<long long>(units, 64LL * cus);
-    const bool zeros = a.mats || a.zero;  // (descriptors in device memory: may have zero points)
-    if (gated) return zeros ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
-    return zeros ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
+    if (gated) return a.zero ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
+    return a.zero ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
 }
 
 }  // namespace
@@ -516,7 +536,7 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W, const uint16_t *x_bf16, 
     a.out_f32 = y_type == QMOE_F32;
     a.activation = activation;
     fill_shape(&a, rows, W->cols, W->group);
-    if (batch > 64) return launch_many(a, (batch + 63) / 64, di.cus, static_cast<hipStream_t>(stream));
+    if (batch > 64) return launch_many(a, di.cus, static_cast<hipStream_t>(stream));
     const int tiles = (batch + 15) / 16, at_once = tiles <= 2 ? tiles : 4;
     return launch_few(a, tiles, (tiles + at_once - 1) / at_once, di.cus, static_cast<hipStream_t>(stream));
 }
@@ -569,7 +589,7 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
         a.items = g.many;
         a.n_items_dev = g.n_many;
         a.max_items = n_tokens / kInt4FewTokens;  // (each has more than that, or stands beside a whole tile)
-        return launch_many(a, a.max_items, di.cus, s);
+        return launch_few(a, 4, a.max_items, di.cus, s);
     };
     if ((st = product()) != QMOE_OK) return st;
     a.mats = wo;
