@@ -629,22 +629,19 @@ qmoe_status layer_workspace_ok(int n_tokens, int n_experts, int d_model, int d_f
     return QMOE_OK;
 }
 
-qmoe_status group_by_expert(const int32_t *expert_idx, int n_tokens, int n_experts, int d_model, int d_ff, int few_tile, int many_from,
-                            void *workspace, float *y, int row_words, hipStream_t s, GroupedTokens *out)
+qmoe_status group_by_expert(const int32_t *expert_idx, int n_tokens, int n_experts, int d_model, int d_ff, int tile, void *workspace,
+                            float *y, int row_words, hipStream_t s, GroupedTokens *out)
 {
     qmoe_ws_layout l;
     const qmoe_status st = qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens, &l);
     if (st != QMOE_OK) return st;
     const LayerPtrs lp = layer_ptrs(workspace, l);
-    MmPlan mp;
-    mp.min_tokens = mp.otherwise = many_from;
-    out->few = lp.items_wi;
-    out->n_few = lp.counters + kCounterFew;
-    out->many = lp.items_mm;
-    out->n_many = lp.counters + kCounterMm;
+    const MmPlan mp;  // (no expert goes to the matrix-core kernel's list)
+    out->items = lp.items_wi;
+    out->n_items = lp.counters + kCounterFew;
     out->perm = lp.perm;
     out->hidden = lp.hidden;
-    return launch_dispatch(dispatch_args(expert_idx, n_tokens, n_experts, row_words, lp, few_tile, few_tile, mp, y), s);
+    return launch_dispatch(dispatch_args(expert_idx, n_tokens, n_experts, row_words, lp, tile, tile, mp, y), s);
 }
 }  // namespace qmoe
 

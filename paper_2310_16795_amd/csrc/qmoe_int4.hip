@@ -5,9 +5,7 @@ namespace qmoe {
 namespace {
 
 constexpr int kInt4MaxSplit = 8;
-constexpr int kInt4FewTokens = 16;  // of an expert: one tile of tokens; those with more get four
-constexpr int kInt4Direct = 4;      // layer calls of up to so many tokens do without the dispatch: an item a token
-constexpr int kInt4AllFew = 64;     // layer calls of up to so many tokens make no tiles but of 16
+constexpr int kInt4Direct = 4;  // layer calls of up to so many tokens do without the dispatch: an item a token
 
 // What both kernels here share.
 //
@@ -160,11 +158,11 @@ __device__ __forceinline__ const uint16_t *int4_x_row(const Int4Args &a, int slo
 
 // Little work: a workgroup's wavefronts share 16 rows (gated: of each projection) along the columns, each with its own piece of LDS for the
 // activations of its block, so that none waits for another before all join their sums, in a fixed order.
-template <int SIDES, int TILES, int PER_BLOCK>
+template <int SIDES, int PER_BLOCK>
 __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Args a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
-    constexpr int TOKENS = 16 * TILES, LD = kInt4BlockCols + 8;  // (16 lanes' reads, a token each, meet no bank twice)
+    constexpr int TOKENS = 16, LD = kInt4BlockCols + 8;  // (16 lanes' reads, a token each, meet no bank twice)
     constexpr int X_BYTES = TOKENS * LD * 2, WAVE_BYTES = X_BYTES + 4 * PER_BLOCK * TOKENS;
     const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n16 = lane & 15, quarter = lane >> 4, from_lane = 4 * (4 * n16 + quarter);
@@ -186,21 +184,19 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 #pragma unroll
         for (int g = 0; g < SIDES; g++) base[g] = 16 * tile, behind[g] = g * a.rows;
         rows.at(a, m, lane, base, behind);
-        const uint16_t *x_row[4 * TILES];
+        const uint16_t *x_row[4];
 #pragma unroll
-        for (int j = 0; j < 4 * TILES; j++)
+        for (int j = 0; j < 4; j++)
             if (4 * j < it.ntok) x_row[j] = int4_x_row(a, it.slot0 + min(4 * j + quarter, it.ntok - 1));
-        u32x4 x_next[4 * TILES], w_next[1][SIDES];
+        u32x4 x_next[4], w_next[1][SIDES];
         auto load_x = [&](int b) {
 #pragma unroll
-            for (int j = 0; j < 4 * TILES; j++)
+            for (int j = 0; j < 4; j++)
                 if (4 * j < it.ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * n16, a.cols, kInt4BlockCols * (b + 1) <= a.cols);
         };
-        f32x4 acc[SIDES][TILES];
+        f32x4 acc[SIDES][1];
 #pragma unroll
-        for (int g = 0; g < SIDES; g++)
-#pragma unroll
-            for (int t = 0; t < TILES; t++) acc[g][t] = (f32x4){0, 0, 0, 0};
+        for (int g = 0; g < SIDES; g++) acc[g][0] = (f32x4){0, 0, 0, 0};
         if (b0 < b1) {
             rows.load(w_next, b0, b1 - 1);
             load_x(b0);
@@ -211,7 +207,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();  // the block before has been read
 #pragma unroll
-            for (int j = 0; j < 4 * TILES; j++) {
+            for (int j = 0; j < 4; j++) {
                 if (4 * j >= it.ntok) continue;
                 *reinterpret_cast<u32x4 *>(&s_x[(4 * j + quarter) * LD + 8 * n16]) = x_next[j];
                 const float all = int4_group_sum<PER_BLOCK>(x_next[j]);
@@ -238,25 +234,21 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
                 rows.load(w_next, b + 1, b1 - 1);
                 load_x(b + 1);
             }
-            int4_block<SIDES, TILES, PER_BLOCK, 1, TOKENS>(acc, w, 0, scale_of, zero_of, bool(m.zero), s_x + n16 * LD + 8 * quarter, LD,
+            int4_block<SIDES, 1, PER_BLOCK, 1, TOKENS>(acc, w, 0, scale_of, zero_of, bool(m.zero), s_x + n16 * LD + 8 * quarter, LD,
                                                            s_sum + 4 * quarter);
         }
         __syncthreads();  // all have read their activations: the sums take their place
 #pragma unroll
-        for (int g = 0; g < SIDES; g++)
-#pragma unroll
-            for (int t = 0; t < TILES; t++) joined[((part * SIDES + g) * TILES + t) * 64 + lane] = acc[g][t];
+        for (int g = 0; g < SIDES; g++) joined[(part * SIDES + g) * 64 + lane] = acc[g][0];
         __syncthreads();
-#pragma unroll
-        for (int t = 0; t < TILES; t++) {
-            if (t % a.split != part || 16 * t >= it.ntok) continue;  // a tile of tokens is joined by one of the wavefronts
+        if (part == 0) {
             f32x4 v[SIDES];
 #pragma unroll
             for (int g = 0; g < SIDES; g++) {
-                v[g] = joined[(g * TILES + t) * 64 + lane];
-                for (int p = 1; p < a.split; p++) v[g] += joined[((p * SIDES + g) * TILES + t) * 64 + lane];
+                v[g] = joined[g * 64 + lane];
+                for (int p = 1; p < a.split; p++) v[g] += joined[(p * SIDES + g) * 64 + lane];
             }
-            int4_results<SIDES>(a, gated, v, t, 16 * tile + n16, quarter, it.slot0, it.ntok, it.none);
+            int4_results<SIDES>(a, gated, v, 0, 16 * tile + n16, quarter, it.slot0, it.ntok, it.none);
         }
         __syncthreads();  // before the next unit's activations overwrite these
     }
@@ -272,7 +264,7 @@ template <int TILES, int PER_BLOCK>
 __global__ __launch_bounds__(256, TILES == 1 ? 4 : 2) void k_int4_tile(const Int4Args a)
 {
     constexpr int TOKENS = 16 * TILES, BLOCKS = 2, COLS = BLOCKS * kInt4BlockCols, LD = COLS + 8, GROUPS = BLOCKS * PER_BLOCK;
-    constexpr int AT_ONCE = TILES == 4 ? 16 : 32, LD_SCALE = AT_ONCE + 8, LD_ZERO = AT_ONCE + 8;
+    constexpr int AT_ONCE = 32, LD_SCALE = AT_ONCE + 8, LD_ZERO = AT_ONCE + 8;
     using Rows = Int4Rows<2, BLOCKS, PER_BLOCK>;
     __shared__ __align__(16) uint16_t s_x[2][TOKENS * LD];
     __shared__ __align__(16) float s_sum[2][BLOCKS * PER_BLOCK * TOKENS];
@@ -419,33 +411,26 @@ void fill_shape(Int4Args *a, int rows, int cols, int group)
     a->blocks_per_group = group < kInt4BlockCols ? 1 : group / kInt4BlockCols;
 }
 
-template <int SIDES, int TILES, int PER_BLOCK>
+template <int SIDES, int PER_BLOCK>
 qmoe_status launch_split_variant(const Int4Args &a, int grid, hipStream_t s)
 {
-    const size_t tokens = 16 * TILES, x = a.split * (tokens * (kInt4BlockCols + 8) * 2 + 4 * PER_BLOCK * tokens);
-    const size_t smem = std::max(x, (size_t)a.split * SIDES * TILES * 64 * sizeof(f32x4));
-    const qmoe_status st = allow_lds(k_int4_split<SIDES, TILES, PER_BLOCK>, smem);
+    const size_t x = a.split * (16 * (kInt4BlockCols + 8) * 2 + 4 * PER_BLOCK * 16);
+    const size_t smem = std::max(x, (size_t)a.split * SIDES * 64 * sizeof(f32x4));
+    const qmoe_status st = allow_lds(k_int4_split<SIDES, PER_BLOCK>, smem);
     if (st != QMOE_OK) return st;
-    hipLaunchKernelGGL((k_int4_split<SIDES, TILES, PER_BLOCK>), dim3(grid), dim3(64 * a.split), smem, s, a);
+    hipLaunchKernelGGL((k_int4_split<SIDES, PER_BLOCK>), dim3(grid), dim3(64 * a.split), smem, s, a);
     QMOE_HIP_TRY(hipGetLastError());
     return QMOE_OK;
 }
-template <int SIDES, int TILES>
-qmoe_status launch_split_tiles(const Int4Args &a, int grid, hipStream_t s)
-{
-    if (a.per_block == 1) return launch_split_variant<SIDES, TILES, 1>(a, grid, s);
-    if (a.per_block == 2) return launch_split_variant<SIDES, TILES, 2>(a, grid, s);
-    return launch_split_variant<SIDES, TILES, 4>(a, grid, s);
-}
 template <int SIDES>
-qmoe_status launch_split_sides(const Int4Args &a, int tiles, int grid, hipStream_t s)
+qmoe_status launch_split(const Int4Args &a, int grid, hipStream_t s)
 {
-    if (tiles <= 1) return launch_split_tiles<SIDES, 1>(a, grid, s);
-    if (tiles <= 2) return launch_split_tiles<SIDES, 2>(a, grid, s);
-    return launch_split_tiles<SIDES, 4>(a, grid, s);
+    if (a.per_block == 1) return launch_split_variant<SIDES, 1>(a, grid, s);
+    if (a.per_block == 2) return launch_split_variant<SIDES, 2>(a, grid, s);
+    return launch_split_variant<SIDES, 4>(a, grid, s);
 }
 template <int TILES>
-qmoe_status launch_tile_variant(const Int4Args &a, int grid, hipStream_t s)
+qmoe_status launch_tile(const Int4Args &a, int grid, hipStream_t s)
 {
     if (a.per_block == 1) hipLaunchKernelGGL((k_int4_tile<TILES, 1>), dim3(grid), dim3(256), 0, s, a);
     else if (a.per_block == 2) hipLaunchKernelGGL((k_int4_tile<TILES, 2>), dim3(grid), dim3(256), 0, s, a);
@@ -454,54 +439,70 @@ qmoe_status launch_tile_variant(const Int4Args &a, int grid, hipStream_t s)
     return QMOE_OK;
 }
 
-// What a call on one of the two kernels takes, us: rounds of workgroups (as many at a time as registers and LDS let a compute unit hold)
-// times a start of 4 and a time a block (split) or a step of two (tile) of one workgroup that is there alone, fitted to single matrices of
-// 1024 x 768, 4096 x 1024, 2080 x 6144 and 12288 x 2080, 1 to 1024 tokens, groups of 128.  Split / tile, measured: 2080 x 6144,
-// 1 token 7.6 / 28.6, 64 23 / 60, 192 45 / 62, 256 65 / 62; 4096 x 1024, 64 9.6 / 16, 128 17 / 17, 256 22 / 17; 12288 x 2080, 1 11 / 13.5,
-// 16 18.6 / 15.1, 64 71 / 28; 1024 x 768, 256 9.8 / 14, 512 17 / 14.
-double split_us(const Int4Args &a, int tiles, long long items, int cus)
+// How a product of up to `tokens` (and no more than 512 or so of one matrix) is split, by what each way takes, us: a start, and rounds of what
+// the compute units hold at a time.  Fitted to single matrices of 384 x 1024, 1024 x 768, 4096 x 1024, 2080 x 6144, 6144 x 2080 and 12288 x 2080,
+// 1 to 1024 tokens, groups of 128.  Measured, k_int4_split / k_int4_tile with 16 tokens an item / with 32: 2080 x 6144, 16 tokens 10 / 32 / 36, 128 30 /
+// 33 / 38, 192 35 / 33 / 39, 512 90 / 55 / 53; 4096 x 1024, 64 8.1 / 9.6 / 11, 128 11 / 9.5 / 11, 512 28 / 18 / 16; 12288 x 2080, 1 8.6 / 13 / -,
+// 16 13 / 15 / 17, 64 27 / 19 / 18, 256 80 / 42 / 32; 1024 x 768, 256 7.3 / 9.0 / 10, 1024 14 / 11 / 11.
+struct Int4Way {
+    double us;
+    int split;  // wavefronts that share a tile's columns (k_int4_split); 0: k_int4_tile
+    int tiles;  // of 16 tokens, an item
+};
+// items: of up to 16 tokens, how many the call has at most
+Int4Way split_way(const Int4Args &a, long long items, int tokens, int cus)
 {
-    const double groups = (double)items * ((a.rows + 15) / 16), held = tiles == 1 ? 2.0 * cus : 1.0 * cus;
-    const int tokens = a.items ? 16 * tiles : std::min(a.batch, 16 * tiles);
-    const double block = (0.55 + 0.04 * tokens) * (tiles == 1 && groups > cus ? 1.6 : 1.0);
-    const double rounds = tiles == 1 ? std::max(1.0, groups / held) : std::ceil(groups / held);
-    return rounds * (4.0 + block * ((a.blocks + kInt4MaxSplit - 1) / kInt4MaxSplit));
-}
-double tile_us(const Int4Args &a, int tiles, long long units, int cus)
-{
-    const double held = tiles == 1 ? 4.0 * cus : 2.0 * cus, step = tiles == 1 ? 1.0 : tiles == 2 ? 1.4 : 2.4;
-    return std::max(1.0, (double)units / held) * (4.0 + step * ((a.blocks + 1) / 2));
-}
-
-// tiles: tiles of 16 tokens of an item; items: how many the call has, at most
-qmoe_status launch_few(Int4Args a, int tiles, long long items, int cus, hipStream_t s)
-{
-    const bool gated = int4_is_gated(a.activation);
-    tiles = tiles <= 2 ? tiles : 4;
-    const long long row_tiles = (a.rows + 15) / 16, tile_units = items * ((a.rows + (gated ? 63 : 127)) / (gated ? 64 : 128));
-    if (a.direct || a.cols < 8 || split_us(a, tiles, items, cus) <= tile_us(a, tiles, tile_units, cus)) {
-        a.split = 1;
-        while (a.split < kInt4MaxSplit && a.split < a.blocks && items * row_tiles * a.split < 16LL * cus) a.split *= 2;
-        const int grid = (int)std::min<long long>(items * row_tiles, 32LL * cus);
-        return gated ? launch_split_sides<2>(a, tiles, grid, s) : launch_split_sides<1>(a, tiles, grid, s);
+    const double groups = (double)items * ((a.rows + 15) / 16);
+    const double block = (0.38 + 0.022 * std::min(tokens, 16)) * (int4_is_gated(a.activation) ? 1.5 : 1.0);
+    Int4Way best{1e30, 1, 1};
+    for (int split = 1; split <= kInt4MaxSplit && (split == 1 || split / 2 < a.blocks); split *= 2) {
+        const double full = groups * split / (16.0 * cus);  // four wavefronts a SIMD
+        const double us = 1.5 + 0.5 * split + std::ceil(full) * (2.0 + block * (1.0 + 0.9 * std::min(1.0, full)) * ((a.blocks + split - 1) / split));
+        if (us < best.us) best = {us, split, 1};
     }
-    const int grid = (int)std::min<long long>(tile_units, 64LL * cus);
-    if (tiles == 1) return launch_tile_variant<1>(a, grid, s);
-    if (tiles == 2) return launch_tile_variant<2>(a, grid, s);
-    return launch_tile_variant<4>(a, grid, s);
+    return best;
+}
+long long tile_units(const Int4Args &a, long long items)
+{
+    return items * (int4_is_gated(a.activation) ? (a.rows + 63) / 64 : (a.rows + 127) / 128);
+}
+Int4Way tile_way(const Int4Args &a, int tiles, long long items, int cus)
+{
+    const double more = std::max(0.0, (double)tile_units(a, items) / cus - 1.0), steps = (a.blocks + 1) / 2;
+    return {tiles == 1 ? 5.5 + steps * (1.08 + 0.58 * more) : 6.0 + steps * (1.3 + 0.8 * more), 0, tiles};
+}
+// of up to 16 tokens an item
+Int4Way narrow_way(const Int4Args &a, long long items, int tokens, int cus)
+{
+    const Int4Way split = split_way(a, items, tokens, cus), tile = tile_way(a, 1, items, cus);
+    return a.direct || a.cols < 8 || split.us <= tile.us ? split : tile;  // (k_int4_tile loads eight columns, and knows no direct items)
+}
+qmoe_status launch_way(Int4Args a, const Int4Way &way, long long items, int cus, hipStream_t s)
+{
+    if (way.split) {
+        a.split = way.split;
+        const int grid = (int)std::min<long long>(items * ((a.rows + 15) / 16), 32LL * cus);
+        return int4_is_gated(a.activation) ? launch_split<2>(a, grid, s) : launch_split<1>(a, grid, s);
+    }
+    const int grid = (int)std::min<long long>(tile_units(a, items), 64LL * cus);
+    return way.tiles == 1 ? launch_tile<1>(a, grid, s) : launch_tile<2>(a, grid, s);
 }
 
-// More tokens of one matrix than a tile: the kernel for many where it fills the GPU one and a half times (12288 x 2080, 256 tokens 39 us, the
-// other way 38; 512 52 / 59; 1024 83 / 102).  In layer calls, where tiles are partly empty, it lost (16 experts of 1024 x 4096, 4001 tokens 213, the
-// other way 205; 64 of 1024 x 2048, 1000 tokens 122 / 99).
-qmoe_status launch_many(const Int4Args &a, int cus, hipStream_t s)
+// One matrix: the kernel for many tokens where it fills the GPU one and a half times (12288 x 2080, 256 tokens 39 us, the other way 32; 512 53 /
+// 56; 1024 84 / 103).  In layer calls, where tiles are partly empty, it lost (16 experts of 1024 x 4096, 4001 tokens 213, the other way 182;
+// 64 of 1024 x 2048, 1000 tokens 122 / 68).
+qmoe_status launch_matrix(const Int4Args &a, int cus, hipStream_t s)
 {
     const bool gated = int4_is_gated(a.activation);
-    const long long items = (a.batch + 63) / 64, units = items * ((a.rows + (gated ? 127 : 255)) / (gated ? 128 : 256));
-    if (2 * units < 3LL * cus || a.cols < 8) return launch_few(a, 4, items, cus, s);
-    const int grid = (int)std::min<long long>(units, 64LL * cus);
-    if (gated) return a.zero ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
-    return a.zero ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
+    const long long units = ((a.batch + 63LL) / 64) * ((a.rows + (gated ? 127 : 255)) / (gated ? 128 : 256));
+    if (a.batch > 64 && 2 * units >= 3LL * cus && a.cols >= 8) {
+        const int grid = (int)std::min<long long>(units, 64LL * cus);
+        if (gated) return a.zero ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
+        return a.zero ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
+    }
+    const long long items = (a.batch + 15) / 16, wide_items = (a.batch + 31) / 32;
+    const Int4Way narrow = narrow_way(a, items, a.batch, cus), wide = tile_way(a, 2, wide_items, cus);
+    return a.batch > 16 && a.cols >= 8 && wide.us < narrow.us ? launch_way(a, wide, wide_items, cus, s) : launch_way(a, narrow, items, cus, s);
 }
 
 }  // namespace
@@ -536,9 +537,7 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W, const uint16_t *x_bf16, 
     a.out_f32 = y_type == QMOE_F32;
     a.activation = activation;
     fill_shape(&a, rows, W->cols, W->group);
-    if (batch > 64) return launch_many(a, di.cus, static_cast<hipStream_t>(stream));
-    const int tiles = (batch + 15) / 16, at_once = tiles <= 2 ? tiles : 4;
-    return launch_few(a, tiles, (tiles + at_once - 1) / at_once, di.cus, static_cast<hipStream_t>(stream));
+    return launch_matrix(a, di.cus, static_cast<hipStream_t>(stream));
 }
 
 qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_matrix *wo, int group, int activation, int n_experts,
@@ -554,56 +553,52 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     hipStream_t s = static_cast<hipStream_t>(stream);
     DeviceInfo di;
     if ((st = gpu_info(&di)) != QMOE_OK) return st;
-    const bool crowded = n_tokens > kInt4AllFew, direct = n_tokens <= kInt4Direct;
+    const bool direct = n_tokens <= kInt4Direct;
+    Int4Args up{}, down{};
+    up.mats = wi;
+    down.mats = wo;
+    up.n_experts = down.n_experts = n_experts;
+    up.activation = activation;
+    fill_shape(&up, d_ff, d_model, group);
+    fill_shape(&down, d_model, d_ff, group);
+    // Experts' tokens in tiles of 16 or of 32, whichever has less to do if every expert leaves a tile partly empty.  (16 / 32, us: 128 experts of 768 x
+    // 3072, 4001 tokens 209 / 175; 16 of 1024 x 4096, 4001 218 / 182; 64 of 1024 x 2048, 1000 Zipf 68 / 73; 32 of 512 x 1024, 400 28 / 31; 256 of
+    // 2080 x 6144, 300 318 / 376.)
+    up.direct = down.direct = direct ? expert_idx : nullptr;
+    long long items = direct ? n_tokens : std::min(n_tokens, n_experts + n_tokens / 16);
+    const int most = direct ? 1 : 16;
+    Int4Way up_way = narrow_way(up, items, most, di.cus), down_way = narrow_way(down, items, most, di.cus);
+    const long long wide_items = std::min(n_tokens, n_experts + n_tokens / 32);
+    const Int4Way up_wide = tile_way(up, 2, wide_items, di.cus), down_wide = tile_way(down, 2, wide_items, di.cus);
+    if (n_tokens > 16 && up_wide.us + down_wide.us < up_way.us + down_way.us) up_way = up_wide, down_way = down_wide, items = wide_items;
     GroupedTokens g{};
     if (direct) {
         qmoe_ws_layout l;
         if ((st = qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens, &l)) != QMOE_OK) return st;
         g.hidden = reinterpret_cast<uint16_t *>(static_cast<unsigned char *>(workspace) + l.hidden);
-    } else if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, kInt4FewTokens,
-                              crowded ? kInt4FewTokens + 1 : 0x7FFFFFFF, workspace, static_cast<float *>(y),
-                              y_type == QMOE_F32 ? d_model : d_model / 2, s, &g)) != QMOE_OK)
+    } else if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, 16 * up_way.tiles, workspace, static_cast<float *>(y),
+                                     y_type == QMOE_F32 ? d_model : d_model / 2, s, &g)) != QMOE_OK) {
         return st;
-    Int4Args a{};
-    a.mats = wi;
-    a.n_experts = n_experts;
-    a.perm = g.perm;
-    a.x = x_bf16;
-    a.ld_x = d_model;
-    a.out = g.hidden;
-    a.ld_out = d_ff;
-    a.out_by_slot = 1;
-    a.activation = activation;
-    fill_shape(&a, d_ff, d_model, group);
-    auto product = [&]() {
-        if (direct) {
-            a.direct = expert_idx;
-            a.max_items = n_tokens;
-            return launch_few(a, 1, n_tokens, di.cus, s);
-        }
-        a.items = g.few;
-        a.n_items_dev = g.n_few;
-        a.max_items = std::min(n_tokens, n_experts + n_tokens / kInt4FewTokens);
-        qmoe_status r = launch_few(a, 1, a.max_items, di.cus, s);
-        if (r != QMOE_OK || !crowded) return r;
-        a.items = g.many;
-        a.n_items_dev = g.n_many;
-        a.max_items = n_tokens / kInt4FewTokens;  // (each has more than that, or stands beside a whole tile)
-        return launch_few(a, 4, a.max_items, di.cus, s);
-    };
-    if ((st = product()) != QMOE_OK) return st;
-    a.mats = wo;
-    a.x = g.hidden;
-    a.ld_x = d_ff;
-    a.x_by_slot = 1;
-    a.out = y;
-    a.ld_out = d_model;
-    a.out_by_slot = 0;
-    a.out_f32 = y_type == QMOE_F32;
-    a.gate = gate;
-    a.activation = QMOE_ACT_NONE;
-    fill_shape(&a, d_model, d_ff, group);
-    return product();
+    }
+    up.perm = down.perm = g.perm;
+    up.items = down.items = g.items;
+    up.n_items_dev = down.n_items_dev = g.n_items;
+    up.max_items = down.max_items = (int)items;
+    up.x = x_bf16;
+    up.ld_x = d_model;
+    up.out = g.hidden;
+    up.ld_out = d_ff;
+    up.out_by_slot = 1;
+    if ((st = launch_way(up, up_way, items, di.cus, s)) != QMOE_OK) return st;
+    down.x = g.hidden;
+    down.ld_x = d_ff;
+    down.x_by_slot = 1;
+    down.out = y;
+    down.ld_out = d_model;
+    down.out_f32 = y_type == QMOE_F32;
+    down.gate = gate;
+    down.activation = QMOE_ACT_NONE;
+    return launch_way(down, down_way, items, di.cus, s);
 }
 
 }  // extern "C"

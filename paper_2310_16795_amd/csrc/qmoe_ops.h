@@ -12,16 +12,16 @@ qmoe_status gpu_info(DeviceInfo *out);
 // Tokens grouped by expert in a layer workspace: the experts with few tokens in tiles of one size (few), the others in tiles of
 // up to kMmTokens (many), the lists' lengths on the device; slot -> token, and the place of the hidden vectors by slot.
 struct GroupedTokens {
-    const Item *few, *many;
-    const int *n_few, *n_many, *perm;
+    const Item *items;
+    const int *n_items, *perm;
     uint16_t *hidden;
 };
 // Sizes and workspace, as the layer calls check them.
 qmoe_status layer_workspace_ok(int n_tokens, int n_experts, int d_model, int d_ff, const void *workspace, size_t workspace_bytes);
-// Enqueues the dispatch kernel on a workspace that is right: experts with fewer than many_from tokens in tiles of up to few_tile.  It
-// also clears the rows (row_words 32-bit words each) of y whose token has no expert.
-qmoe_status group_by_expert(const int32_t *expert_idx, int n_tokens, int n_experts, int d_model, int d_ff, int few_tile, int many_from,
-                            void *workspace, float *y, int row_words, hipStream_t s, GroupedTokens *out);
+// Enqueues the dispatch kernel on a workspace that is right: every expert's tokens in tiles of up to `tile`.  It also clears the rows
+// (row_words 32-bit words each) of y whose token has no expert.
+qmoe_status group_by_expert(const int32_t *expert_idx, int n_tokens, int n_experts, int d_model, int d_ff, int tile, void *workspace,
+                            float *y, int row_words, hipStream_t s, GroupedTokens *out);
 
 constexpr int kMaxJoined = 16;      // rows of a token that are joined, or copies of one: k and copies
 constexpr int kMaxInt4Rows = 1 << 24;

@@ -1,4 +1,4 @@
-"""Calls of the operators on their CPU build (cpu_build.py), seeded: `python cases.py KIND SEED COUNT`.  Prints each call before it is
+"""Calls of the operators on their CPU build (operators_build.py), seeded: `python operator_calls.py KIND SEED COUNT`.  Prints each call before it is
 made and what came of it; the exit code is 1 when an access was out of range or a result wrong."""
 import ctypes
 import os

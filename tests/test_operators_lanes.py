@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 def library(tmp_path_factory):
     import importlib.util
 
-    spec = importlib.util.spec_from_file_location("operators_cpu_build", os.path.join(HERE, "operators", "cpu_build.py"))
+    spec = importlib.util.spec_from_file_location("operators_build", os.path.join(HERE, "operators", "operators_build.py"))
     mod = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(mod)
     return mod.build(str(tmp_path_factory.mktemp("operators")))
@@ -22,6 +22,6 @@ def library(tmp_path_factory):
 
 @pytest.mark.parametrize("kind,count", [("norm", 60), ("route", 60), ("int4", 60), ("layer", 30)])
 def test_results_and_every_access(library, kind, count):
-    cmd = [sys.executable, os.path.join(HERE, "operators", "cases.py"), kind, "1", str(count)]
+    cmd = [sys.executable, os.path.join(HERE, "operators", "operator_calls.py"), kind, "1", str(count)]
     r = subprocess.run(cmd, env={**os.environ, "QMOE_LIBRARY": library}, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600)
     assert r.returncode == 0 and r.stdout.rstrip().endswith("done"), r.stdout[-3000:]
