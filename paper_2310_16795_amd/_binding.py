@@ -380,6 +380,15 @@ def qmoe_bf16_layer_forward(wi_ptrs, wo_ptrs, n_experts: int, d_model: int, d_ff
 _TYPES: dict = {}  # torch dtype -> QMOE_F32 / QMOE_BF16 (16-bit integers stand for bf16 bits)
 
 
+def _here(*tensors) -> None:
+    """The call is enqueued on the current device: its tensors must be there."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensor on device {t.device}, but the current one is {here}" if t.is_cuda else "device tensor expected")
+
+
 def _types() -> dict:
     if not _TYPES:
         import torch
@@ -387,6 +396,15 @@ def _types() -> dict:
         if hasattr(torch, "uint16"):
             _TYPES[torch.uint16] = BF16
     return _TYPES
+
+
+def _here(*tensors) -> None:
+    """A call is enqueued on the current device: its tensors must be there."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is {here}")
 
 
 def _matrix(t, rows: int, cols: int, what: str):
@@ -440,10 +458,12 @@ def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, pos
     n, d = h.shape
     hp, ht, hl = _matrix(h, n, d, "h")
     yp, yt, yl = (0, 0, 0) if y is None else _matrix(y, n * k, d, "y")
+    _here(h, y, h_out, x, gate, channel_scale)
     op, ot, ol = (0, ht, 0) if h_out is None else _matrix(h_out, n, d, "h_out")
     xp, xl = (0, 0) if x is None else _bf16_matrix(x, n * copies, d, "x")
     if ot != ht:
         raise ValueError("h_out must be of h's type")
+    _here(h, y, h_out, x, gate, channel_scale)
     _check(lib().qmoe_residual_norm(hp, ht, hl, yp, yt, yl, k, _vector(gate, n * k, "gate"), _norm_ptr(post, d, "post"), alpha,
                                     _vector(channel_scale, d, "channel_scale"), _norm_ptr(pre, d, "pre"), op, ol, xp, xl, copies, n, d,
                                     _stream_ptr(stream)), "qmoe_residual_norm")
@@ -461,6 +481,8 @@ def qmoe_route(logits, expert_idx, gate, bias=None, token_mask=None, gates: int 
         raise ValueError("expert_idx must be int32")
     if token_mask is not None and (token_mask.numel() != n or token_mask.element_size() != 1):
         raise ValueError("token_mask must hold a byte for every token")
+    _here(logits, expert_idx, gate, bias, token_mask)
+    _here(logits, expert_idx, gate, bias, token_mask)
     _check(lib().qmoe_route(lp, lt, ld, _vector(bias, n_experts, "bias"), _dev_ptr(token_mask), n, n_experts, shape[1], gates,
                             _dev_ptr(expert_idx), _vector(gate, n * shape[1], "gate"), _stream_ptr(stream)), "qmoe_route")
 
@@ -510,6 +532,7 @@ def qmoe_int4_matvec(W: qmoe_int4_matrix, x_bf16, y, activation: int = ACT_NONE,
     batch, rows = x_bf16.shape[0], W.rows
     xp, xl = _bf16_matrix(x_bf16, batch, W.cols, "x")
     yp, yt, yl = _matrix(y, batch, rows // 2 if activation >= ACT_SILU_GATED else rows, "y")
+    _here(x_bf16, y)
     _check(lib().qmoe_int4_matvec(byref(W), xp, xl, batch, activation, yp, yt, yl, _stream_ptr(stream)), "qmoe_int4_matvec")
 
 
@@ -519,13 +542,14 @@ def qmoe_int4_layer_forward(wi_dev, wo_dev, group: int, activation: int, n_exper
     n_tokens = x_bf16.shape[0]
     xp, xl = _bf16_matrix(x_bf16, n_tokens, d_model, "x")
     yp, yt, yl = _matrix(y, n_tokens, d_model, "y")
-    if expert_idx.numel() != n_tokens or expert_idx.element_size() != 4:
+    if expert_idx.numel() != n_tokens or expert_idx.element_size() != 4 or expert_idx.is_floating_point():
         raise ValueError("expert_idx must be int32, one for every token")
     if xl != d_model or yl != d_model:
         raise ValueError("contiguous tensor expected")
     need = _INT4_BYTES * n_experts
     if wi_dev.numel() * wi_dev.element_size() < need or wo_dev.numel() * wo_dev.element_size() < need:
         raise ValueError("expert descriptor arrays too small")
+    _here(wi_dev, wo_dev, x_bf16, expert_idx, gate, y, workspace)
     _check(lib().qmoe_int4_layer_forward(_dev_ptr(wi_dev), _dev_ptr(wo_dev), group, activation, n_experts, d_model, d_ff, xp,
                                          _dev_ptr(expert_idx), _vector(gate, n_tokens, "gate"), n_tokens, yp, yt, _dev_ptr(workspace),
                                          workspace.numel() * workspace.element_size(), _stream_ptr(stream)),

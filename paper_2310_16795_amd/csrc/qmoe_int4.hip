@@ -261,10 +261,10 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 // The scales and zero points of AT_ONCE groups go through LDS, too, a wavefront's own: a row's few bytes a step, asked for step by step, would
 // be the same lines of memory again and again, gone from the caches in between.
 template <int TILES, int PER_BLOCK>
-__global__ __launch_bounds__(256, TILES == 1 ? 4 : 2) void k_int4_tile(const Int4Args a)
+__global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int4Args a)
 {
     constexpr int TOKENS = 16 * TILES, BLOCKS = 2, COLS = BLOCKS * kInt4BlockCols, LD = COLS + 8, GROUPS = BLOCKS * PER_BLOCK;
-    constexpr int AT_ONCE = 32, LD_SCALE = AT_ONCE + 8, LD_ZERO = AT_ONCE + 8;
+    constexpr int AT_ONCE = TILES == 1 ? 32 : 16, LD_SCALE = AT_ONCE + 8, LD_ZERO = AT_ONCE + 8;
     using Rows = Int4Rows<2, BLOCKS, PER_BLOCK>;
     __shared__ __align__(16) uint16_t s_x[2][TOKENS * LD];
     __shared__ __align__(16) float s_sum[2][BLOCKS * PER_BLOCK * TOKENS];
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 2) void k_int4_tile(const Int
         u32x4 w_next[BLOCKS][2];
         rows.load(w_next, 0, a.blocks - 1);
         load_x(0);
-        // groups g0 .. g0 + AT_ONCE - 1 of the wavefront's 32 rows: eight lanes a row, eight groups a lane
+        // groups g0 .. g0 + AT_ONCE - 1 of the wavefront's 32 rows, eight groups a lane
         auto fill = [&](int g0) {
             constexpr int LANES = AT_ONCE / 8, AT = 64 / LANES;  // lanes of a row, rows at a time
 #pragma unroll
@@ -305,6 +305,7 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 2) void k_int4_tile(const Int
                 const int r = AT * j + lane / LANES, at = 8 * (lane % LANES), side = r >> 4;
                 const int base = gated ? first : first + 16 * side;
                 const size_t row = (size_t)(min(base + (r & 15), a.rows - 1) + (gated ? side * a.rows : 0)) * a.groups;
+                if (g0 + at >= PER_BLOCK * a.blocks) continue;  // (nothing behind the last block is read)
                 uint16_t *to = &s_scale[wave][r * LD_SCALE + at];
                 uint8_t *to_zero = &s_zero[wave][r * LD_ZERO + at];
                 if (g0 + at + 8 <= a.groups) {

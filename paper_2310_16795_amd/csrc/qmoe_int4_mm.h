@@ -29,30 +29,18 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
     const int n16 = lane & 15, quarter = lane >> 4, from_lane = 4 * (4 * n16 + quarter);
     const int piece = threadIdx.x & 15, stager = threadIdx.x >> 4;  // stages 8 columns of tokens stager + 16 t
     const int row_blocks = (a.rows + 64 * OUT_TILES - 1) / (64 * OUT_TILES);
-    const int n_items = a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
+    const int n_items = (a.batch + TOKENS - 1) / TOKENS;
     const long long total = (long long)n_items * row_blocks;
     const size_t row_bytes = (size_t)64 * a.blocks;
     for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
-        // Workgroups go to the eight XCDs in turn: an XCD's units follow each other, and those of a whole matrix go by eight tiles of
-        // tokens, so that what it holds at a time shares rows and activations in its L2.
-        long long at = unit;
-        int item, rb;
-        if (a.items) {
-            item = (int)(at / row_blocks), rb = (int)(at - (long long)item * row_blocks);
-        } else {
-            const long long whole = total / 8 * 8;
-            if (at < whole) at = (at & 7) * (whole / 8) + (at >> 3);
-            const int tiles8 = n_items / 8;  // whole groups of eight tiles
-            const int group = (int)(at / (8LL * row_blocks)), in = (int)(at - group * 8LL * row_blocks);
-            const int wide = group < tiles8 ? 8 : n_items - 8 * tiles8;
-            rb = in / wide, item = 8 * group + in % wide;
-        }
-        int expert = 0, slot0 = item * TOKENS, ntok = min(TOKENS, a.batch - slot0);
-        if (a.items) {
-            const Item it = a.items[item];
-            expert = it.expert, slot0 = it.slot0, ntok = min(it.ntok, TOKENS);
-        }
-        const Int4Matrix m = int4_matrix(a, expert);
+        // Workgroups go to the eight XCDs in turn: an XCD's units follow each other and go by eight tiles of tokens, so that what it holds at a
+        // time shares rows and activations in its L2.
+        const long long whole = total / 8 * 8, at = unit < whole ? (unit & 7) * (whole / 8) + (unit >> 3) : unit;
+        const int tiles8 = n_items / 8;  // whole groups of eight tiles
+        const int group = (int)(at / (8LL * row_blocks)), in = (int)(at - group * 8LL * row_blocks);
+        const int wide = group < tiles8 ? 8 : n_items - 8 * tiles8;
+        const int rb = in / wide, token0 = (8 * group + in % wide) * TOKENS, ntok = min(TOKENS, a.batch - token0);
+        const Int4Matrix m = int4_matrix(a, 0);
         const int first = 16 * OUT_TILES * (4 * rb + wave);  // row of this wavefront
         // the matrix's row that a tile's row is
         auto row_of = [&](int r, int in_tile) {
@@ -63,10 +51,7 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
         for (int r = 0; r < kMmRows; r++) w_row[r] = m.weights + row_of(r, lane >> 2) * row_bytes + 16 * (lane & 3);
         const uint16_t *x_row[kMmTiles];
 #pragma unroll
-        for (int t = 0; t < kMmTiles; t++) {
-            const int slot = slot0 + min(16 * t + stager, ntok - 1);
-            x_row[t] = a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
-        }
+        for (int t = 0; t < kMmTiles; t++) x_row[t] = a.x + (size_t)(token0 + min(16 * t + stager, ntok - 1)) * a.ld_x;
         u32x4 x_next[kMmTiles], w_next[kMmRows];
         auto load = [&](int blk) {
 #pragma unroll
@@ -184,15 +169,13 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
             for (int i = 0; i < 4; i++) {
                 const int in_tile = 16 * t + 4 * quarter + i;
                 if (in_tile >= ntok) continue;
-                const int token = a.perm ? a.perm[slot0 + in_tile] : slot0 + in_tile;
-                const float gate = a.gate ? a.gate[token] : 1.0f;
 #pragma unroll
                 for (int r = 0; r < OUT_TILES; r++) {
                     const int row = first + 16 * r + n16;
                     if (row >= a.rows) continue;
                     float v = acc[r][t][i];
                     if constexpr (GATED) v = int4_gated(v, acc[r + OUT_TILES][t][i], a.activation);
-                    int4_store(a, a.out_by_slot ? slot0 + in_tile : token, gate, row, v);
+                    int4_store(a, token0 + in_tile, 1.0f, row, v);
                 }
             }
         }
