@@ -209,6 +209,19 @@ def test_int4_matvec(gpu, rows, cols, batch, group, zeros, act, yt, pad, whole):
         assert np.linalg.norm(d) <= 2e-6 * np.linalg.norm(want) + 1e-30
 
 
+INT4_MANY = [  # rows, cols, batch, group, zeros, activation, y: enough work for the kernels of 16, 32 and 64 tokens a tile
+    *((12000, 600, batch, group, zeros, act, yt) for batch in (33, 300) for group, zeros, act, yt in (
+        (128, True, "none", "f32"), (64, False, "gelu", "bf16"), (32, True, "silu", "f32"), (32, False, "relu", "bf16"), (256, True, "none", "bf16"))),
+    *((1601, 200, 3601, group, zeros, "none", "f32") for group in (32, 64, 128) for zeros in (False, True)),
+    *((3202, 330, 3590, group, zeros, act, yt) for group, act, yt in ((32, "silu", "f32"), (64, "gelu", "bf16"), (256, "silu", "f32")) for zeros in (False, True)),
+]
+
+
+@pytest.mark.parametrize("rows,cols,batch,group,zeros,act,yt", INT4_MANY)
+def test_int4_matvec_of_much_work(gpu, rows, cols, batch, group, zeros, act, yt):
+    test_int4_matvec(gpu, rows, cols, batch, group, zeros, act, yt, 0, act in ("none", "relu"))
+
+
 @pytest.mark.parametrize("batch", [3, 40, 200])
 def test_int4_tokens_that_are_not_finite(gpu, batch):
     rng = np.random.default_rng(batch)
@@ -357,3 +370,94 @@ def test_block_step_in_a_graph_and_on_another_stream(gpu):
             assert torch.equal(b[n], eager[n]), (turn, n)
             if turn == 0:
                 assert torch.equal(b[n], on_side[n]), n
+
+
+def test_two_streams_at_once(gpu):
+    """Two programs with their own workspaces, each on a stream, give what each gives alone."""
+    made = [_block(gpu, np.random.default_rng(seed), *sizes) for seed, sizes in ((3, (300, 8, 512, 1024, 2)), (4, (41, 16, 384, 640, 4)))]
+    results = ("x", "logits", "idx", "gate", "y", "out", "next")
+    alone = []
+    for _, _, _, b, step in made:
+        step()
+        torch.cuda.synchronize()
+        alone.append({n: b[n].clone() for n in results})
+    streams = [torch.cuda.Stream() for _ in made]
+    for (_, _, _, b, _), s in zip(made, streams):
+        for n in results:
+            b[n].zero_()
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        for (_, _, _, _, step), s in zip(made, streams):
+            step(s)
+    torch.cuda.synchronize()
+    for (_, _, _, b, _), want in zip(made, alone):
+        for n in results:
+            assert torch.equal(b[n], want[n]), n
+
+
+# ---------------------------------------------------------------- offsets past 32 bits
+
+def _far(n, d, gpu, dtype):
+    """A matrix whose rows are so far apart that the last begins more than 2^32 bytes behind the first"""
+    step = (2 ** 32 // dtype.itemsize + 1024) // (n - 1)
+    return torch.empty(step * (n - 1) + d, dtype=dtype, device=gpu).as_strided((n, d), (step, 1))
+
+
+def test_rows_far_apart(gpu):
+    rng = np.random.default_rng(8)
+    n, d = 3, 200
+    h, x = torch.from_numpy(rng.standard_normal((n, d)).astype(np.float32)).to(gpu), torch.empty((n, d), dtype=torch.bfloat16, device=gpu)
+    near_h = torch.empty_like(h)
+    pre = dev.DeviceNorm("layer", eps=1e-5)
+    q.qmoe_residual_norm(h, h, near_h, x, pre=pre)
+    far_h, far_out, far_x = _far(n, d, gpu, torch.float32), _far(n, d, gpu, torch.float32), _far(n, d, gpu, torch.bfloat16)
+    far_h.copy_(h)
+    q.qmoe_residual_norm(far_h, far_h, far_out, far_x, pre=pre)
+    assert torch.equal(far_out, near_h) and torch.equal(far_x, x)
+    idx, gate = torch.empty((2, n, 4), dtype=torch.int32, device=gpu), torch.empty((2, n, 4), device=gpu)
+    q.qmoe_route(h, idx[0], gate[0])
+    q.qmoe_route(far_h, idx[1], gate[1])
+    assert torch.equal(idx[0], idx[1]) and torch.equal(gate[0], gate[1])
+    M = _matrix(gpu, _weights(rng, 96, d, 64, True, False), d, 64)
+    y, far_y = torch.empty((n, 96), device=gpu), _far(n, 96, gpu, torch.float32)
+    q.qmoe_int4_matvec(M.desc, x, y)
+    q.qmoe_int4_matvec(M.desc, far_x, far_y)
+    assert torch.equal(y, far_y)
+
+
+@pytest.mark.parametrize("batch", [1, 20])
+def test_int4_matrix_of_more_than_32_bits(gpu, batch):
+    rows, cols, group = 2 ** 20 + 300, 8192, 128
+    weights = torch.randint(0, 256, (rows, cols // 2), dtype=torch.uint8, device=gpu)
+    scale = (0.5 + torch.rand((rows, cols // group), device=gpu)).half().view(torch.int16)
+    x, x64 = _up(np.random.default_rng(2).standard_normal((batch, cols)) / 64, gpu, "bf16")
+    y = torch.empty((batch, rows), device=gpu)
+    q.qmoe_int4_matvec(dev.DeviceInt4Matrix(weights, scale, cols, group).desc, x, y)
+    for r0 in (0, 2 ** 19, rows - 300):
+        values = q.qmoe_int4_unpack_host(weights[r0:r0 + 300].cpu().numpy(), cols)
+        want, err = plain.int4_product(x64, values, scale[r0:r0 + 300].cpu().numpy().view(np.uint16), None, group, "none")
+        _near(y[:, r0:r0 + 300], want, err, "f32", f"rows from {r0} on")
+
+
+# ---------------------------------------------------------------- what is refused before anything is enqueued
+
+def test_refusals_of_tensors(gpu):
+    f = lambda *s, t=torch.float32, d=gpu: torch.zeros(s, dtype=t, device=d)  # noqa: E731
+    b16, i32 = torch.bfloat16, torch.int32
+    M = _matrix(gpu, _weights(np.random.default_rng(0), 32, 64, 32, False, True), 64, 32).desc
+    bad = [
+        lambda: q.qmoe_residual_norm(f(4, 8), f(4, 8, d="cpu"), f(4, 8)), lambda: q.qmoe_residual_norm(f(4, 8), f(4, 7), f(4, 8)),
+        lambda: q.qmoe_residual_norm(f(4, 8), f(4, 8), f(4, 8, t=b16)), lambda: q.qmoe_residual_norm(f(8, 4).t(), f(4, 8), f(4, 8)),
+        lambda: q.qmoe_residual_norm(f(4, 8, t=torch.float16), x=f(4, 8, t=b16)), lambda: q.qmoe_residual_norm(f(4, 8), x=f(4, 8)),
+        lambda: q.qmoe_residual_norm(f(4, 8), x=f(4, 8, t=b16), pre=dev.DeviceNorm("rms", f(9))), lambda: q.qmoe_residual_norm(f(4, 8), f(8, 8), f(4, 8), k=2, gate=f(7)),
+        lambda: q.qmoe_route(f(4, 8), f(4, 2, t=i32), f(4, 3)), lambda: q.qmoe_route(f(4, 8), f(4, 2), f(4, 2)),
+        lambda: q.qmoe_route(f(4, 8), f(4, 2, t=i32), f(4, 2), bias=f(7)), lambda: q.qmoe_route(f(4, 8), f(4, 2, t=i32), f(4, 2), token_mask=f(4)),
+        lambda: q.qmoe_int4_matvec(M, f(2, 63, t=b16), f(2, 32)), lambda: q.qmoe_int4_matvec(M, f(2, 64), f(2, 32)),
+        lambda: q.qmoe_int4_matvec(M, f(2, 64, t=b16), f(2, 32), activation=q.ACTIVATIONS["silu"]), lambda: q.qmoe_int4_matvec(M, f(2, 64, t=b16), f(2, 32, t=torch.float16)),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i} was taken")
+    with pytest.raises(q.QmoeError):
+        q.qmoe_route(f(4, 8), f(4, 9, t=i32), f(4, 9))
