@@ -153,12 +153,21 @@ def weights(rng, rows, cols, group, zeros, whole):
     return values, packed, s.astype(np.float16).view(np.uint16), zero
 
 
-def int4(rng, i):
+def int4_many(rng, i):
+    """Rows and tokens enough for the kernels that take 16, 32 or 64 tokens of a matrix at a time."""
+    rows, cols = int(rng.integers(200, 700)), int(rng.choice([8, 64, 130, 200, 390]))
+    return int4(rng, i, (rows, cols, [20, 40, 70, 66, 130, 97][i % 6]))
+
+
+def int4(rng, i, sizes=None):
     m = Memory(i % 2)
     act = ["none", "none", "relu", "silu", "gelu"][i % 5]
     rows, cols = int(np.exp(rng.uniform(0, np.log(90)))), int(np.exp(rng.uniform(0, np.log(1100))))
     rows += rows % 2 if act in ("silu", "gelu") else 0
     batch = int(rng.choice([1, 2, 15, 16, 17, 33, 50, 65, 130])) if i % 4 else 1
+    if sizes:
+        rows, cols, batch = sizes
+        rows -= rows % 2
     group, zeros, yt, whole = int(rng.choice([32, 64, 128, 256, 384])), rng.random() < 0.5, int(rng.integers(0, 2)), i % 2 == 0
     values, packed, s, zero = weights(rng, rows, cols, group, zeros, whole)
     results = rows // 2 if act in ("silu", "gelu") else rows
@@ -176,10 +185,17 @@ def int4(rng, i):
     return st == 0 and kept and near(got, want, err, yt, "y")
 
 
-def layer(rng, i):
+def layer_many(rng, i):
+    """Hidden vectors and tokens enough for tiles of 16 or 32 tokens of an expert."""
+    return layer(rng, i, (int(rng.choice([1, 2, 4])), int(rng.choice([20, 60, 150])), 8 * int(rng.integers(1, 20)), 8 * int(rng.integers(30, 60))))
+
+
+def layer(rng, i, sizes=None):
     m = Memory(i % 2)
     act, E, T = ["relu", "silu", "gelu"][i % 3], int(rng.choice([1, 2, 5, 9])), int(np.exp(rng.uniform(0, np.log(150))))
     d_model, d_ff = (8 * int(rng.integers(1, 24)) for _ in range(2))
+    if sizes:
+        E, T, d_model, d_ff = sizes
     group, yt = int(rng.choice([32, 64, 128])), int(rng.integers(0, 2))
     rows_i = d_ff if act == "relu" else 2 * d_ff
     ex = [[weights(rng, r, c, group, rng.random() < 0.5, False) for r, c in ((rows_i, d_model), (d_model, d_ff))] for _ in range(E)]
@@ -223,7 +239,7 @@ if __name__ == "__main__":
     rng, ok = np.random.default_rng(seed), True
     for i in range(count):
         before = L.lanes_reports()
-        right = {"norm": norm, "route": route, "int4": int4, "layer": layer}[kind](rng, i)
+        right = {"norm": norm, "route": route, "int4": int4, "int4_many": int4_many, "layer": layer, "layer_many": layer_many}[kind](rng, i)
         out = L.lanes_reports() - before
         ok &= bool(right) and out == 0
         if not right or out:

@@ -20,8 +20,10 @@ def library(tmp_path_factory):
     return mod.build(str(tmp_path_factory.mktemp("operators")))
 
 
-@pytest.mark.parametrize("kind,count", [("norm", 60), ("route", 60), ("int4", 60), ("layer", 30)])
-def test_results_and_every_access(library, kind, count):
+# on a GPU of so many compute units: few make a call one of much work
+@pytest.mark.parametrize("kind,count,units", [("norm", 60, 6), ("route", 60, 6), ("int4", 60, 6), ("int4_many", 36, 1), ("int4_many", 30, 6), ("layer", 30, 6),
+                                              ("layer_many", 18, 3)])
+def test_results_and_every_access(library, kind, count, units):
     cmd = [sys.executable, os.path.join(HERE, "operators", "operator_calls.py"), kind, "1", str(count)]
-    r = subprocess.run(cmd, env={**os.environ, "QMOE_LIBRARY": library}, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600)
+    r = subprocess.run(cmd, env={**os.environ, "QMOE_LIBRARY": library, "LANES_COMPUTE_UNITS": str(units)}, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600)
     assert r.returncode == 0 and r.stdout.rstrip().endswith("done"), r.stdout[-3000:]
