@@ -135,10 +135,11 @@ __device__ __forceinline__ float int4_group_sum(u32x4 x)
 
 inline bool int4_is_gated(int activation) { return activation == QMOE_ACT_SILU_GATED || activation == QMOE_ACT_GELU_GATED; }
 
+// (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z)): both are g / (1 + exp(-t)), and nothing cancels.
 __device__ __forceinline__ float int4_gated(float g, float u, int activation)
 {
-    if (activation == QMOE_ACT_SILU_GATED) return g / (1.0f + expf(-g)) * u;
-    return 0.5f * g * (1.0f + tanhf(0.7978845608028654f * fmaf(0.044715f * g * g, g, g))) * u;
+    const float t = activation == QMOE_ACT_SILU_GATED ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
+    return g / (1.0f + expf(-t)) * u;
 }
 
 __device__ __forceinline__ void int4_store(const Int4Args &a, size_t out_row, float gate, int r, float v)
