@@ -512,7 +512,7 @@ qmoe_status qmoe_residual_norm(const void *h /*device*/, int h_type, size_t ld_h
  * answer with a zero row.  token_mask (device, one byte a token, 0 = padding; NULL = none): all k places of a
  * masked token get -1 and 0; its logits are not read.
  * ld: elements from a token's logits to the next one's, at least n_experts.
- * One launch, no workspace.
+ * One launch, no workspace.  Up to 2048 experts the logits cross memory once; beyond that they are read again for each of the k.
  * Errors: INVALID_ARG (NULL, a size < 1, k > n_experts, an unknown type or kind, ld < n_experts), LIMIT (n_experts > 16384, n_tokens > 2^20,
  * k > 16), HIP.
  */
@@ -582,7 +582,8 @@ qmoe_status qmoe_int4_quantize_host(const float *w /*host [rows][cols]*/, int ro
  * (y_type), ld_y elements apart, overwritten; rows behind the last token and columns behind the last one are left as they were.
  * Products are exact, sums fp32; a group's sum is scaled in fp32; one rounding at the end if y is bf16.
  * An activation that is not finite spoils its own token only: every result of that token may be NaN.
- * One launch, no workspace.
+ * One launch, no workspace.  Which kernel, and how the columns are split, follows from rows, cols and batch, and so does the order of
+ * the fp32 sums: a token's results can differ in their last bits between batch sizes, never between two calls of one size.
  * Errors: INVALID_ARG (NULL, a size < 1, weights not 16-byte aligned, a group that is none, reserved not 0, an unknown type or
  * activation, a gated one with odd rows, ld_x < cols, ld_y less than the results of a token), LIMIT (rows > 2^24, cols > 2^20, batch > 2^20), HIP.
  */
@@ -598,7 +599,8 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W /*host*/, const uint16_t 
  * outside [0, n_experts), experts without tokens: as there.  y: device [n_tokens][d_model] fp32 or bf16 (y_type), 4-byte aligned,
  * overwritten; apart from x, expert_idx and gate.  workspace: as there, qmoe_moe_layer_workspace(n_experts, d_model, d_ff, n_tokens) bytes.  An activation that is not
  * finite spoils its own token only.
- * Enqueues three kernels on `stream`: the dispatch and one per product; no second stream, no events.
+ * Enqueues on `stream` the dispatch and a kernel for each product; up to four tokens the two products alone (a token's
+ * slot in the workspace's hidden vectors is then its number, and the dispatch's part is not written).  No second stream, no events.
  * Calls that share a workspace must not overlap.
  * Errors: INVALID_ARG (also d_model or d_ff not divisible by 8), WORKSPACE, LIMIT (as there; d_ff, d_model <= 32768), HIP.
  */

@@ -380,15 +380,6 @@ def qmoe_bf16_layer_forward(wi_ptrs, wo_ptrs, n_experts: int, d_model: int, d_ff
 _TYPES: dict = {}  # torch dtype -> QMOE_F32 / QMOE_BF16 (16-bit integers stand for bf16 bits)
 
 
-def _here(*tensors) -> None:
-    """The call is enqueued on the current device: its tensors must be there."""
-    import torch
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError(f"tensor on device {t.device}, but the current one is {here}" if t.is_cuda else "device tensor expected")
-
-
 def _types() -> dict:
     if not _TYPES:
         import torch
@@ -398,10 +389,18 @@ def _types() -> dict:
     return _TYPES
 
 
+def _current_device() -> int:
+    """The current GPU's number, as torch.cuda.current_device() has it once torch has started the GPU (that asks whether it has each time)."""
+    global _current_device
+    import torch
+    device = torch.cuda.current_device()
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return device
+
+
 def _here(*tensors) -> None:
     """A call is enqueued on the current device: its tensors must be there."""
-    import torch
-    here = torch.cuda.current_device()
+    here = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the current device is {here}")
@@ -458,7 +457,6 @@ def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, pos
     n, d = h.shape
     hp, ht, hl = _matrix(h, n, d, "h")
     yp, yt, yl = (0, 0, 0) if y is None else _matrix(y, n * k, d, "y")
-    _here(h, y, h_out, x, gate, channel_scale)
     op, ot, ol = (0, ht, 0) if h_out is None else _matrix(h_out, n, d, "h_out")
     xp, xl = (0, 0) if x is None else _bf16_matrix(x, n * copies, d, "x")
     if ot != ht:
@@ -481,7 +479,6 @@ def qmoe_route(logits, expert_idx, gate, bias=None, token_mask=None, gates: int 
         raise ValueError("expert_idx must be int32")
     if token_mask is not None and (token_mask.numel() != n or token_mask.element_size() != 1):
         raise ValueError("token_mask must hold a byte for every token")
-    _here(logits, expert_idx, gate, bias, token_mask)
     _here(logits, expert_idx, gate, bias, token_mask)
     _check(lib().qmoe_route(lp, lt, ld, _vector(bias, n_experts, "bias"), _dev_ptr(token_mask), n, n_experts, shape[1], gates,
                             _dev_ptr(expert_idx), _vector(gate, n * shape[1], "gate"), _stream_ptr(stream)), "qmoe_route")

@@ -13,7 +13,11 @@ namespace {
 // them, so that decoding one tile runs beside multiplying the one before and few registers hold operands.  Two wavefronts a SIMD: the
 // sums (64 registers) are scaled into the result (64) in fp32, which accumulation registers could not take part in.
 // With PER_BLOCK groups of 128 / PER_BLOCK columns, a group's sum starts at -(16 + z) * sum of x (formed by those who stage x).
-// Scales and zero points of AT_ONCE groups lie in LDS, a wavefront's own.
+// Scales and zero points of kMmAtOnce groups lie in LDS, a wavefront's own.
+// 12288 x 2080 (gated, groups of 128), 4001 tokens: 263 us, 780 TFLOP/s; the matrix cores are busy for 86 us of it, vector instructions (decoding 34 %,
+// scaling 15, group sums and epilogue the rest) for 137, and the two overlap in part.  The library's bf16 product of that shape is 196 us, without the activation.
+// Without gain: operands straight from memory, other orders of tokens and rows, wave priorities, matrix and vector
+// instructions interleaved by hand (282 then).
 constexpr int kMmRows = 4, kMmTiles = 4, kMmAtOnce = 32;
 
 template <bool GATED, bool ZEROS, int PER_BLOCK>
