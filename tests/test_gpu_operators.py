@@ -395,6 +395,41 @@ def test_two_streams_at_once(gpu):
             assert torch.equal(b[n], want[n]), n
 
 
+@pytest.mark.parametrize("T,k", [(1, 2), (40, 2), (300, 4)])
+def test_block_step_on_ternary_experts(gpu, T, k):
+    """The router's choice feeds the compressed layer, and the stream takes the rows that it leaves."""
+    from paper_2310_16795_amd import synth
+
+    w = synth.WORKLOADS["switch_base128"].scaled(n_experts=8, d_model=256, d_ff=512, n_tokens=8)
+    dd = dev.DeviceDict(device=gpu)
+    layer = dev.DeviceLayer(w.n_experts, w.d_model, w.d_ff, gpu)
+    for e in range(w.n_experts):
+        for which, tern, scale in (("wi", w.wi_ternary(e), w.wi_scale(e)), ("wo", w.wo_ternary(e), w.wo_scale(e))):
+            layer.set_expert(e, which, *q.qmoe_encode_host(dd.handle, tern), scale)
+    layer.finalize(device_order_of=dd)
+    rng = np.random.default_rng(T)
+    h, h64 = _up(rng.standard_normal((T, 256)), gpu)
+    logits, _ = _up(rng.standard_normal((T, 8)), gpu)
+    mask = torch.ones(T, dtype=torch.uint8, device=gpu)
+    mask[T // 2:T // 2 + T // 4] = 0
+    x = torch.empty((T * k, 256), dtype=torch.bfloat16, device=gpu)
+    y, out = torch.empty((T * k, 256), device=gpu), torch.empty((T, 256), device=gpu)
+    idx, gate = torch.empty((T, k), dtype=torch.int32, device=gpu), torch.empty((T, k), device=gpu)
+    q.qmoe_residual_norm(h, x=x, pre=dev.DeviceNorm("rms"), copies=k)
+    q.qmoe_route(logits, idx, gate, token_mask=mask, gates=q.GATES_CHOSEN)
+    layer.forward(dd, x.view(torch.int16), idx, y, layer.workspace(T * k))
+    q.qmoe_residual_norm(h, y, out, k=k, gate=gate)
+    # the same layer call with the choice made on the host
+    want, _, _ = plain.route(logits.cpu().numpy(), None, mask.cpu().numpy(), k, 1)
+    y_host = torch.empty_like(y)
+    layer.forward(dd, x.view(torch.int16), torch.from_numpy(want.astype(np.int32).reshape(-1)).to(gpu), y_host, layer.workspace(T * k))
+    assert torch.equal(y, y_host) and y.isfinite().all() and y.any()
+    assert not y[idx.view(-1) < 0].any() and torch.equal((idx < 0).all(1), mask == 0)
+    want, err, _, _ = plain.residual_norm(h64, y.cpu().numpy().astype(np.float64), k, gate.cpu().numpy().reshape(-1), None, 1.0, None, None, 1)
+    _near(out, want, err, "f32", "out")
+    dd.close()
+
+
 # ---------------------------------------------------------------- offsets past 32 bits
 
 def _far(n, d, gpu, dtype):
