@@ -14,8 +14,8 @@ constexpr int kInt4Direct = 4;  // layer calls of up to so many tokens do withou
 // instructions a pair.  What the zero points (and the 16) take off is (16 + z) * sum of x over the group, where a group's sum starts;
 // the sums of x are formed by those who bring x into LDS.
 // Four neighbouring lanes load the 64 bytes that a row has in a block (one access of the cache; a load in the operands' order, a row a
-// lane, is four), and ds_bpermute brings them to their lanes.  A lane's scales come for BLOCKS blocks at a time, those of the next 4 * BLOCKS in one
-// load, a quarter of the wavefront each.
+// lane, is four), and ds_bpermute brings them to their lanes.  In k_int4_split the scales of the next four blocks come in one load, a
+// quarter of the wavefront each; k_int4_tile keeps them in LDS.
 
 // SIDES tiles of 16 rows: their weights and scales, as a lane loads them.
 template <int SIDES, int BLOCKS, int PER_BLOCK>
@@ -158,7 +158,7 @@ __device__ __forceinline__ const uint16_t *int4_x_row(const Int4Args &a, int slo
 
 // Little work: a workgroup's wavefronts share 16 rows (gated: of each projection) along the columns, each with its own piece of LDS for the
 // activations of its block, so that none waits for another before all join their sums, in a fixed order.
-// Bound by latency: 4096 x 1024, one token (2.2 MB) 5.2 us, of which a launch that does nothing is 2.4; 2080 x 6144 with zero points, 37 tokens (7.1 MB) 13 us,
+// Bound by latency: 4096 x 1024, one token (2.2 MB) 5.2 us (k_route of one token, a launch with next to no work, is 2.2 in the same trace); 2080 x 6144 with zero points, 37 tokens (7.1 MB) 13 us,
 // six blocks one after the other in each of 3120 wavefronts, 2080 x 6144 with one token 7.4 us (0.9 TB/s).  Two tiles of rows a wavefront (half the
 // activations' reads) lost wherever this kernel is taken (2080 x 6144, 16 tokens 9.9 -> 12, 64 tokens 17.6 -> 19).
 template <int SIDES, int PER_BLOCK>
