@@ -18,7 +18,7 @@ struct RouteArgs {
 
 // A logit as the operator counts it: masked (-infinity) if it is NaN, finite if it is +infinity.
 __device__ __forceinline__ float counted(float l) { return l == l ? fminf(l, FLT_MAX) : -INFINITY; }
-__device__ __forceinline__ float key_of(float l, float bias) { return l == -INFINITY ? l : counted(l + bias); }
+__device__ __forceinline__ float key_of(float l, float bias) { return counted(l + bias); }  // (of a masked l: -infinity, or NaN, which counts as that)
 
 template <int TYPE>
 __device__ __forceinline__ float logit(const void *base, size_t at)
@@ -120,8 +120,10 @@ __device__ __forceinline__ void four_logits(float (&v)[4], const void *base, siz
 // A token's keys lie in the registers of LANES lanes, four neighbouring experts in a lane's four registers, then those 4 * LANES further: one
 // pass over memory.  Each of the k rounds takes the largest key (a reduction over the lanes), of equal ones that of the lowest
 // index (a second one), and the lane that held it looks for its next best.
-// With many experts memory bounds it: 4096 tokens of 2048 fp32 logits (34 MB) 9.4 us, 3.6 TB/s; with few the rounds do, k reductions
-// one after the other: 16384 tokens of 256 bf16 logits, best eight, 10.7 us for 9.4 MB.  16 lanes a token up to 256 experts keep the reductions inside
+// With many experts memory bounds it: 4096 tokens of 2048 fp32 logits (34 MB) 9.4 us, 3.6 TB/s; with few instruction issue
+// does: 16384 tokens of 256 bf16 logits, best eight, 10.7 us for 9.4 MB, 1280 vector instructions a wavefront of four tokens (8.5 us), two thirds of them
+// looking for the next best of 16 keys.  Keeping each lane's second best, too, was 17: with eight of 16 lanes' keys to take, some lane of four tokens needs
+// its third in nearly every round.  16 lanes a token up to 256 experts keep the reductions inside
 // a row of the wavefront (four DPP steps) and four tokens in one instruction.
 template <int TYPE, int LANES, int PER, bool BIAS>
 __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
