@@ -265,7 +265,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 // be the same lines of memory again and again, gone from the caches in between.
 // Few tokens an expert: memory, 64 tokens on 57 of 256 gated experts of 2080 x 6144 (1.17 GB) 260 us for both products, 4.5 TB/s where a large copy has 4.9.
 // More: the vector instructions of decoding and scaling and each unit's start, 128 experts of 768 x 3072, 4001 tokens (38 GFLOP, 310 MB) 163 us:
-// vector instructions take 43 of a product's 76 us, the matrix cores 13.  32 tokens a tile at three wavefronts a SIMD 167, at two 174.
+// vector instructions take 43 us of the first product and 32 of the second (70-76 each), the matrix cores 13.  32 tokens a tile at three wavefronts a SIMD 167, at two 174.
 template <int TILES, int PER_BLOCK>
 __global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int4Args a)
 {

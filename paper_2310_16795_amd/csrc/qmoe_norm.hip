@@ -79,9 +79,9 @@ __device__ __forceinline__ void store8(void *base, size_t at, int c, int d, cons
 // barrier) or are one row's.  The sums of a norm (of the values, then of the squares around the mean: no difference of
 // two large sums) go through DPP and, with several wavefronts, LDS; their order depends on the sizes alone.
 //
-// Bound by memory: 2048 tokens of 2080 values (bf16 h, two fp32 rows a token, 68 MB) 14.6 us, 4.7 TB/s, what a large copy reaches; 8191 of 768 (fp32 h
-// written back, bf16 y, both norms, 101 MB) 25.5 us, 3.9 TB/s: rows of 768 are two wavefronts, the second half empty.  One token is
-// the launch (3 us).  Rows of 768 with a wavefront of two or four times as many values gained nothing.
+// Bound by memory: 2048 tokens of 2080 values (bf16 h, two fp32 rows a token, 68 MB) 14.6 us, 4.7 TB/s, what a large copy reaches; 8191 of 1024 (fp32 h
+// written back, bf16 y, two layer norms, 101 MB) 25.5 us, 3.9 TB/s: a row's four sums come one after the other, and its loads and stores
+// do not overlap them.  One token is the launch (3 us).  Rows of 1024 with a wavefront of two or four times as many values gained nothing.
 template <int HT, int YT, int PER, bool ALONE>
 __global__ __launch_bounds__(ALONE ? 256 : 1024) void k_residual_norm(const NormArgs a)
 {
