@@ -512,7 +512,7 @@ qmoe_status qmoe_residual_norm(const void *h /*device*/, int h_type, size_t ld_h
  * answer with a zero row.  token_mask (device, one byte a token, 0 = padding; NULL = none): all k places of a
  * masked token get -1 and 0; its logits are not read.
  * ld: elements from a token's logits to the next one's, at least n_experts.
- * One launch, no workspace.  Up to 2048 experts the logits cross memory once; beyond that they are read again for each of the k.
+ * One launch, no workspace.
  * Errors: INVALID_ARG (NULL, a size < 1, k > n_experts, an unknown type or kind, ld < n_experts), LIMIT (n_experts > 16384, n_tokens > 2^20,
  * k > 16), HIP.
  */

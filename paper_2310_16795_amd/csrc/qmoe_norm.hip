@@ -91,6 +91,10 @@ __global__ __launch_bounds__(ALONE ? 256 : 1024) void k_residual_norm(const Norm
     const long long row = alone ? (long long)blockIdx.x * (blockDim.x >> 6) + wave : blockIdx.x;
     if (row >= a.n_tokens) return;  // (a workgroup of one row leaves as one)
     const int me = alone ? lane : (int)threadIdx.x, step = 64 * a.waves * 8;
+    // the longest rows fill the registers: their quarters are not to be loaded ahead of each other (512 rows of 32768 54 us, spilled 97)
+    auto apart = [] {
+        if constexpr (PER == 4) __builtin_amdgcn_sched_barrier(0);
+    };
     int at_sum = 0;
     auto row_sum = [&](float v) {
         v = wave_sum(v);
@@ -137,12 +141,13 @@ __global__ __launch_bounds__(ALONE ? 256 : 1024) void k_residual_norm(const Norm
 #pragma unroll
                 for (int i = 0; i < 8; i++) v[p].v[i] += w.v[i];
             }
+            apart();
         }
     };
 
     Eight h[PER];
 #pragma unroll
-    for (int p = 0; p < PER; p++) h[p] = load8<HT>(a.h, (size_t)row * a.ld_h, 8 * me + p * step, a.d);
+    for (int p = 0; p < PER; p++) h[p] = load8<HT>(a.h, (size_t)row * a.ld_h, 8 * me + p * step, a.d), apart();
     if (a.y) {
         Eight b[PER];
 #pragma unroll
@@ -158,6 +163,7 @@ __global__ __launch_bounds__(ALONE ? 256 : 1024) void k_residual_norm(const Norm
                 const Eight y = load8<YT>(a.y, r * a.ld_y, 8 * me + p * step, a.d);
 #pragma unroll
                 for (int i = 0; i < 8; i++) b[p].v[i] = fmaf(g, y.v[i], b[p].v[i]);
+                apart();
             }
         }
         if (a.has_post) norm(b, a.post);
@@ -173,6 +179,7 @@ __global__ __launch_bounds__(ALONE ? 256 : 1024) void k_residual_norm(const Norm
             // a norm's mean and bias, or an infinite gate, must not reach the columns from d on
 #pragma unroll
             for (int i = 0; i < 8; i++) h[p].v[i] = 8 * me + p * step + i < a.d ? h[p].v[i] : 0.0f;
+            apart();
         }
     }
     if (a.h_out) {

@@ -192,55 +192,82 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
     if (t < a.n_tokens) finish<TYPE, LANES>(a, t, l, mine, top, sum);
 }
 
-// More experts than registers hold: a workgroup a token, the logits read again for every round (from L2 as a rule): the
-// largest key behind the last one taken, in the order (key down, index up).
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_route_wide(const RouteArgs a)
+// More experts than a wavefront's registers hold: a workgroup a token, its keys in the registers of 512 lanes.  The rounds are k_route's, joined over the
+// wavefronts through LDS, one barrier each (two places in turn).  4096 tokens of 4096 experts, best eight: 61 us; 64 of 16384: 12; reading the
+// logits again for every round took 119 and 119.
+constexpr int kWideLanes = 512;
+
+template <int TYPE, int PER>
+__global__ __launch_bounds__(kWideLanes) void k_route_wide(const RouteArgs a)
 {
-    __shared__ float s_val[4];
-    __shared__ int s_idx[4];
+    constexpr int WAVES = kWideLanes / 64;
+    __shared__ float s_top[WAVES], s_sum[WAVES], s_val[2][WAVES];
+    __shared__ int s_idx[2][WAVES];
     const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const bool there = !(a.mask && a.mask[t] == 0);
-    auto all_max = [&](float v) {
-        v = lanes_max<64>(v);
-        __syncthreads();
-        if (lane == 0) s_val[wave] = v;
-        __syncthreads();
-        return fmaxf(fmaxf(s_val[0], s_val[1]), fmaxf(s_val[2], s_val[3]));
-    };
-    float top = 0.0f, sum = 0.0f;
-    const size_t row = (size_t)t * a.ld;
-    if (there && !a.chosen) {
-        top = -INFINITY;
-        for (int e = threadIdx.x; e < a.n_experts; e += 256) top = fmaxf(top, counted(logit<TYPE>(a.logits, row + e)));
-        top = all_max(top);
-        for (int e = threadIdx.x; e < a.n_experts; e += 256) {
-            const float v = counted(logit<TYPE>(a.logits, row + e));
-            sum += v == -INFINITY ? 0.0f : expf(v - top);
-        }
-        sum = lanes_sum<64>(sum);
-        __syncthreads();
-        if (lane == 0) s_val[wave] = sum;
-        __syncthreads();
-        sum = (s_val[0] + s_val[1]) + (s_val[2] + s_val[3]);
+    auto expert = [&](int i) { return 4 * (int)threadIdx.x + 4 * kWideLanes * (i >> 2) + (i & 3); };
+    float key[PER];
+#pragma unroll
+    for (int i = 0; i < PER; i += 4) {
+        float q[4];
+        four_logits<TYPE>(q, a.logits, (size_t)t * a.ld, expert(i), a.n_experts, there);
+#pragma unroll
+        for (int j = 0; j < 4; j++) key[i + j] = counted(q[j]);
     }
-    float last = INFINITY;
-    int last_e = -1, mine = -1;
-    for (int j = 0; there && j < a.k; j++) {
-        float best = -INFINITY;
-        int best_e = 0x7FFFFFFF;
-        for (int e = threadIdx.x; e < a.n_experts; e += 256) {
-            const float v = key_of(counted(logit<TYPE>(a.logits, row + e)), a.bias ? a.bias[e] : 0.0f);
-            if ((v < last || (v == last && e > last_e)) && v > best) best = v, best_e = e;
-        }
-        const float m = all_max(best);
-        const int e = lanes_min<64>(best == m ? best_e : 0x7FFFFFFF);
-        if (lane == 0) s_idx[wave] = e;
+    float top = 0.0f, sum = 0.0f;
+    if (!a.chosen) {
+        top = key[0];
+#pragma unroll
+        for (int i = 1; i < PER; i++) top = fmaxf(top, key[i]);
+        top = lanes_max<64>(top);
+        if (lane == 0) s_top[wave] = top;
         __syncthreads();
-        last = m;
-        last_e = min(min(s_idx[0], s_idx[1]), min(s_idx[2], s_idx[3]));
+        for (int w = 0; w < WAVES; w++) top = fmaxf(top, s_top[w]);
+        top = fmaxf(top, -FLT_MAX);
+#pragma unroll
+        for (int i = 0; i < PER; i++) sum += share(key[i], top);
+        sum = lanes_sum<64>(sum);
+        if (lane == 0) s_sum[wave] = sum;
+        __syncthreads();
+        sum = 0.0f;
+        for (int w = 0; w < WAVES; w++) sum += s_sum[w];
+    }
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < PER; i += 4) {
+            float q[4];
+            four_logits<QMOE_F32>(q, a.bias, 0, expert(i), a.n_experts, true);
+#pragma unroll
+            for (int j = 0; j < 4; j++) key[i + j] = key_of(key[i + j], q[j]);
+        }
+    }
+    float best = key[0];
+    int best_i = 0, mine = -1;
+#pragma unroll
+    for (int i = 1; i < PER; i++)
+        if (key[i] > best) best = key[i], best_i = i;
+    for (int j = 0; j < a.k; j++) {
+        float m = lanes_max<64>(best);
+        int e = lanes_min<64>(best == m ? expert(best_i) : 0x7FFFFFFF);
+        if (lane == 0) s_val[j & 1][wave] = m, s_idx[j & 1][wave] = e;
+        __syncthreads();
+        for (int w = 0; w < WAVES; w++) {
+            const float v = s_val[j & 1][w];
+            const int at = s_idx[j & 1][w];
+            e = v > m || (v == m && at < e) ? at : e;
+            m = fmaxf(m, v);
+        }
         if (m == -INFINITY) break;  // the same for the whole workgroup
-        if (lane == j) mine = last_e;
+        if (lane == j) mine = e;
+        if (e == expert(best_i)) {  // one lane
+            best = -INFINITY;
+            const int gone = best_i;
+#pragma unroll
+            for (int i = 0; i < PER; i++) {
+                if (i == gone) key[i] = -INFINITY;
+                if (key[i] > best) best = key[i], best_i = i;
+            }
+        }
     }
     if (wave == 0) finish<TYPE, 64>(a, t, lane, mine, top, sum);
 }
@@ -253,6 +280,8 @@ void launch_per(const RouteArgs &a, hipStream_t s)
     else hipLaunchKernelGGL((k_route<TYPE, LANES, PER, false>), dim3(grid), dim3(256), 0, s, a);
 }
 
+static_assert(kMaxExperts <= 32 * kWideLanes, "k_route_wide holds every key");
+
 template <int TYPE>
 qmoe_status launch_route(const RouteArgs &a, hipStream_t s)
 {
@@ -263,7 +292,9 @@ qmoe_status launch_route(const RouteArgs &a, hipStream_t s)
     else if (e <= 512) launch_per<TYPE, 64, 8>(a, s);
     else if (e <= 1024) launch_per<TYPE, 64, 16>(a, s);
     else if (e <= 2048) launch_per<TYPE, 64, 32>(a, s);
-    else hipLaunchKernelGGL((k_route_wide<TYPE>), dim3(a.n_tokens), dim3(256), 0, s, a);
+    else if (e <= 8 * kWideLanes) hipLaunchKernelGGL((k_route_wide<TYPE, 8>), dim3(a.n_tokens), dim3(kWideLanes), 0, s, a);
+    else if (e <= 16 * kWideLanes) hipLaunchKernelGGL((k_route_wide<TYPE, 16>), dim3(a.n_tokens), dim3(kWideLanes), 0, s, a);
+    else hipLaunchKernelGGL((k_route_wide<TYPE, 32>), dim3(a.n_tokens), dim3(kWideLanes), 0, s, a);
     QMOE_HIP_TRY(hipGetLastError());
     return QMOE_OK;
 }

@@ -111,7 +111,7 @@ def norm(rng, i):
 def route(rng, i):
     m = Memory(i % 2)
     n = int(rng.choice([1, 3, 18, 37]))
-    e = int(np.exp(rng.uniform(0, np.log(2300)))) if i % 5 else int(rng.choice([1, 64, 65, 256, 512, 2049]))
+    e = int(np.exp(rng.uniform(0, np.log(2300)))) if i % 5 else int(rng.choice([1, 64, 65, 256, 512, 2049, 4099, 8200]))
     n = min(n, 4) if e > 1000 else n
     k, lt, chosen = min(e, int(rng.choice([1, 2, 5, 8, 16]))), int(rng.integers(0, 2)), int(rng.integers(0, 2))
     l = 2 * rng.standard_normal((n, e))

@@ -127,6 +127,8 @@ ROUTES = [  # tokens, experts, k, logits, chosen, bias, masked share, padding, k
     (64, 257, 4, "f32", 0, True, 0.0, 0, "masked"), (31, 512, 2, "bf16", 1, False, 0.2, 5, "masked"), (40, 1000, 8, "f32", 1, True, 0.0, 0, "special"),
     (50, 2048, 1, "f32", 0, False, 0.0, 0, "normal"), (9, 2049, 5, "bf16", 0, True, 0.2, 1, "equal"), (6, 16384, 16, "f32", 1, False, 0.0, 0, "special"),
     (1025, 8, 2, "f32", 1, False, 0.0, 0, "lowest"), (8, 7, 7, "bf16", 0, True, 0.0, 0, "special"),
+    (20, 4096, 8, "f32", 0, True, 0.1, 0, "equal"), (7, 4099, 16, "bf16", 0, True, 0.0, 1, "masked"), (5, 8192, 8, "bf16", 1, False, 0.3, 0, "lowest"),
+    (6, 8193, 3, "f32", 0, True, 0.0, 2, "special"), (4, 16383, 16, "bf16", 0, False, 0.0, 0, "equal"),
 ]
 
 
