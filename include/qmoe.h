@@ -599,7 +599,7 @@ qmoe_status qmoe_int4_matvec(const qmoe_int4_matrix *W /*host*/, const uint16_t 
  * outside [0, n_experts), experts without tokens: as there.  y: device [n_tokens][d_model] fp32 or bf16 (y_type), 4-byte aligned,
  * overwritten; apart from x, expert_idx and gate.  workspace: as there, qmoe_moe_layer_workspace(n_experts, d_model, d_ff, n_tokens) bytes.  An activation that is not
  * finite spoils its own token only.
- * Enqueues on `stream` the dispatch and a kernel for each product; up to four tokens the two products alone (a token's
+ * Enqueues on `stream` the dispatch and a kernel for each product; up to eight tokens the two products alone (a token's
  * slot in the workspace's hidden vectors is then its number, and the dispatch's part is not written).  No second stream, no events.
  * Calls that share a workspace must not overlap.
  * Errors: INVALID_ARG (also d_model or d_ff not divisible by 8), WORKSPACE, LIMIT (as there; d_ff, d_model <= 32768), HIP.

@@ -215,7 +215,7 @@ def layer(rng, i, sizes=None):
     print(f"layer {i}: {E} experts {d_model} x {d_ff}, {T} tokens, group {group} act {act} y {yt}", flush=True)
     st = L.qmoe_int4_layer_forward(*descs, group, q.ACTIVATIONS[act], E, d_model, d_ff, x_at, m.put(idx), m.put(gate), T, y_at, yt, ws, n_ws, None)
     lay = q.qmoe_moe_layer_ws_layout(E, d_model, d_ff, T)
-    order = np.argsort(np.where((idx < 0) | (idx >= E), E, idx), kind="stable") if T > 4 else np.arange(T)  # slot -> token (few tokens: as they are)
+    order = np.argsort(np.where((idx < 0) | (idx >= E), E, idx), kind="stable") if T > 8 else np.arange(T)  # slot -> token (few tokens: as they are)
     hidden = plain.of_bits(read(ws + lay.hidden, T * d_ff, np.uint16)).reshape(T, d_ff)
     y = read_rows(y_at, T, d_model, d_model, yt)[0]
     ok, none = st == 0, (idx < 0) | (idx >= E)

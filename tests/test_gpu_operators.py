@@ -244,7 +244,8 @@ LAYERS = [  # experts, d_model, d_ff, tokens, group, zeros, activation, y, gate,
     (12, 256, 520, 40, 128, False, "relu", "f32", True, "uniform"), (7, 136, 264, 300, 32, True, "gelu", "bf16", False, "crowded"),
     (3, 512, 384, 700, 128, True, "silu", "f32", True, "crowded"), (64, 128, 256, 64, 64, False, "relu", "bf16", True, "uniform"),
     (4, 768, 640, 1500, 128, False, "relu", "bf16", True, "uniform"), (9, 72, 88, 33, 64, False, "relu", "f32", False, "none"),
-    (2000, 64, 64, 100, 32, True, "relu", "f32", True, "uniform"),
+    (2000, 64, 64, 100, 32, True, "relu", "f32", True, "uniform"), (3, 264, 392, 8, 128, True, "gelu", "f32", True, "crowded"), (3, 264, 392, 9, 128, True, "gelu", "f32", True, "crowded"),
+    (40, 128, 72, 8, 64, False, "relu", "bf16", False, "uniform"), (40, 128, 72, 9, 64, False, "relu", "bf16", False, "none"), (2, 64, 64, 8, 32, False, "silu", "bf16", True, "none"),
 ]
 
 
@@ -262,7 +263,7 @@ def _check_layer(ex, x64, idx, gate, group, act, yt, y, ws, d_model, d_ff):
     """Each expert's hidden vectors as the workspace holds them, and the results from those (a value next to a rounding border
     may go either way in the first product; the second is held to what the first wrote)."""
     E, T = len(ex), idx.size
-    order = np.argsort(np.where((idx < 0) | (idx >= E), E, idx), kind="stable") if T > 4 else np.arange(T)  # slot -> token (few tokens: as they are)
+    order = np.argsort(np.where((idx < 0) | (idx >= E), E, idx), kind="stable") if T > 8 else np.arange(T)  # slot -> token (few tokens: as they are)
     lay = q.qmoe_moe_layer_ws_layout(E, d_model, d_ff, T)
     hidden = plain.of_bits(ws.cpu().numpy()[lay.hidden:lay.hidden + 2 * T * d_ff].view(np.uint16)).reshape(T, d_ff)
     none = (idx < 0) | (idx >= E)
