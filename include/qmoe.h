@@ -580,7 +580,8 @@ qmoe_status qmoe_int4_quantize_host(const float *w /*host [rows][cols]*/, int ro
  *   y[b][r] = act( sum over groups of s * sum over the group's columns of (q - z) * x[b][c] ),  b < batch
  * x: device bf16, ld_x elements from a token to the next (>= cols, any alignment that fits the type).  y: device fp32 or bf16
  * (y_type), ld_y elements apart, overwritten; rows behind the last token and columns behind the last one are left as they were.
- * Products are exact, sums fp32; a group's sum is scaled in fp32; one rounding at the end if y is bf16.
+ * Products are exact, sums fp32; a group's sum is scaled in fp32; one rounding at the end if y is bf16.  q - z is formed first: a weight of 0 takes nothing from its
+ * activation however large that is.  Sums are kept at a sixteenth, so that no product of a finite activation overflows.
  * An activation that is not finite spoils its own token only: every result of that token may be NaN.
  * One launch, no workspace.  Which kernel, and how the columns are split, follows from rows, cols and batch, and so does the order of
  * the fp32 sums: a token's results can differ in their last bits between batch sizes, never between two calls of one size.

@@ -75,17 +75,40 @@ __device__ __forceinline__ void int4_load_packed(uint32_t (&v)[WORDS], P from)
     }
 }
 
-// Eight weights (a word) as bf16 16 + q, in the order of their columns: bits 3..6 of a bf16 between 16 and 32 are its
-// units, so a shift and an and-or do for two, exactly.  The 16 goes with the zero point, against the sum of x.
-// The two constants are hidden from the compiler, which knows no and-or with literals (and takes three instructions).
-__device__ __forceinline__ bf16x8 int4_plus16(uint32_t w)
+// Eight weights (a word) as bf16 (q - z) / 16, in the order of their columns.  Exact, so that a weight of 0 takes nothing from its activation however large
+// that is, and below 1, so that no product of a finite activation overflows; a group's scale brings the 16 back.
+// Four bits under the exponent of 1024 are a binary16 number 1024 + q or, four bits higher up, 1024 + 16 q; a mixed-precision multiply-add takes either
+// to (q - z) / 16 in fp32, whose upper half is the bf16: 17 instructions a word.  (16 + q as bf16, its excess taken off with the sum of x, was eight: the two
+// large sums cancel, and one activation of 10^4 on a weight of 0 cost a group of ordinary ones 1e-3 of its sum.)
+// The constants are hidden from the compiler, which knows no and-or with literals (and takes three instructions).
+struct Int4Zero {
+    float low, high;  // what the two places take off
+};
+__device__ __forceinline__ Int4Zero int4_zero(uint32_t z)
 {
-    uint32_t m = 0x00780078u, b = 0x41804180u;
+    const float s = 0.0625f * (float)z;
+    return {-64.0f - s, -4.0f - s};
+}
+__device__ __forceinline__ bf16x8 int4_weights(uint32_t w, Int4Zero zero)
+{
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    uint32_t m = 0x000F000Fu, m16 = 0x00F000F0u, b = 0x64006400u;
     asm("" : "+s"(m));
+    asm("" : "+s"(m16));
     asm("" : "+v"(b));
-    const u32x4 v = {((w << 3) & m) | b, ((w >> 1) & m) | b, ((w >> 5) & m) | b, ((w >> 9) & m) | b};
+    const uint32_t w8 = w >> 8;
+    const uint32_t halves[4] = {(w & m) | b, (w & m16) | b, (w8 & m) | b, (w8 & m16) | b};
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const f16x2 h = __builtin_bit_cast(f16x2, halves[i]);
+        const float unit = i % 2 ? 0.00390625f : 0.0625f, off = i % 2 ? zero.high : zero.low;
+        const float lo = fmaf((float)h[0], unit, off), hi = fmaf((float)h[1], unit, off);
+        v[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    }
     return __builtin_bit_cast(bf16x8, v);
 }
+__device__ __forceinline__ float int4_scale(uint16_t s) { return 16.0f * half_bits_to_float(s); }
 
 // Eight activations of a token from column c on, 0 from column cols on.  whole: none is missing (the same for the wavefront).  The other
 // path is rare, and is kept from asking for registers that the loop around it needs.
@@ -116,21 +139,6 @@ __device__ __forceinline__ u32x4 int4_x_end(u32x4 v, int c, int cols)
     if (over & 4) v = (u32x4){v[2], v[3], 0u, 0u};
     if (over & 8) v = (u32x4){0u, 0u, 0u, 0u};
     return v;
-}
-
-// The sum of x over a group, in the last of the lanes (of 16 that hold the 128 columns of a token's block) whose columns the group is.
-template <int PER_BLOCK>
-__device__ __forceinline__ float int4_group_sum(u32x4 x)
-{
-    const bf16x2 one = __builtin_bit_cast(bf16x2, 0x3F803F80u);
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; i++) s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)x[i]), one, s, false);
-    s += dpp_f<0x111, 0xf>(0.0f, s);
-    s += dpp_f<0x112, 0xf>(0.0f, s);
-    if constexpr (PER_BLOCK <= 2) s += dpp_f<0x114, 0xf>(0.0f, s);
-    if constexpr (PER_BLOCK == 1) s += dpp_f<0x118, 0xf>(0.0f, s);
-    return s;
 }
 
 inline bool int4_is_gated(int activation) { return activation == QMOE_ACT_SILU_GATED || activation == QMOE_ACT_GELU_GATED; }

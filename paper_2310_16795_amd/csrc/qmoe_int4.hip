@@ -12,9 +12,8 @@ constexpr int kInt4Direct = 8;
 // What both kernels here share.
 //
 // v_mfma_f32_16x16x32_bf16 takes 16 tokens as its first operand and 16 rows as its second, so a result lane holds one
-// row and four tokens and needs one scale.  16 bytes of a row are a lane's operands for four steps of 32 columns and become 16 + q with two
-// instructions a pair.  What the zero points (and the 16) take off is (16 + z) * sum of x over the group, where a group's sum starts;
-// the sums of x are formed by those who bring x into LDS.
+// row and four tokens and needs one scale.  16 bytes of a row are a lane's operands for four steps of 32 columns and become (q - z) / 16
+// (int4_weights); a lane's weights are one row's, so a group's zero point is one for the lane.
 // Four neighbouring lanes load the 64 bytes that a row has in a block (one access of the cache; a load in the operands' order, a row a
 // lane, is four), and ds_bpermute brings them to their lanes.  In k_int4_split the scales of the next four blocks come in one load, a
 // quarter of the wavefront each; k_int4_tile keeps them in LDS.
@@ -74,28 +73,29 @@ struct Int4Rows {
     }
 };
 
-// A block's 128 columns: acc += scale * (sum over the group of (16 + q) x - (16 + z) * sum of x), tokens and rows of this wavefront.
-// x: this lane's first operand in LDS, a token's row every ld_x values; sums: the block's [group][token], this lane's four tokens.
-template <int SIDES, int TILES, int PER_BLOCK, int BLOCKS, int TOKENS>
+// A block's 128 columns: acc += scale * sum over the group of (q - z) x, tokens and rows of this wavefront.
+// x: this lane's first operand in LDS, a token's row every ld_x values.
+template <int SIDES, int TILES, int PER_BLOCK, int BLOCKS>
 __device__ __forceinline__ void int4_block(f32x4 (&acc)[SIDES][TILES], const u32x4 (&w)[SIDES], int u, const uint32_t (&scale_of)[SIDES][Int4Rows<SIDES, BLOCKS, PER_BLOCK>::WORDS],
                                            const uint32_t (&zero_of)[SIDES][Int4Rows<SIDES, BLOCKS, PER_BLOCK>::ZERO_WORDS], bool zeros,
-                                           const uint16_t *x, int ld_x, const float *sums)
+                                           const uint16_t *x, int ld_x)
 {
     f32x4 sum[SIDES][TILES];
+    Int4Zero zero[SIDES];
 #pragma unroll
     for (int s = 0; s < 4; s++) {
-        const int in_block = s * PER_BLOCK / 4, i = u * PER_BLOCK + in_block;
+        const int i = u * PER_BLOCK + s * PER_BLOCK / 4;
         if (s * PER_BLOCK % 4 == 0) {
 #pragma unroll
             for (int g = 0; g < SIDES; g++) {
-                const float zero = zeros ? -16.0f - (float)((zero_of[g][i / 4] >> (8 * (i % 4))) & 255u) : -24.0f;
+                zero[g] = int4_zero(zeros ? (zero_of[g][i / 4] >> (8 * (i % 4))) & 255u : 8u);
 #pragma unroll
-                for (int t = 0; t < TILES; t++) sum[g][t] = zero * *reinterpret_cast<const f32x4 *>(sums + in_block * TOKENS + 16 * t);
+                for (int t = 0; t < TILES; t++) sum[g][t] = (f32x4){0, 0, 0, 0};
             }
         }
         bf16x8 wf[SIDES];
 #pragma unroll
-        for (int g = 0; g < SIDES; g++) wf[g] = int4_plus16(w[g][s]);
+        for (int g = 0; g < SIDES; g++) wf[g] = int4_weights(w[g][s], zero[g]);
 #pragma unroll
         for (int t = 0; t < TILES; t++) {
             const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(x + 16 * t * ld_x + 32 * s);
@@ -105,7 +105,7 @@ __device__ __forceinline__ void int4_block(f32x4 (&acc)[SIDES][TILES], const u32
         if ((s + 1) * PER_BLOCK % 4) continue;
 #pragma unroll
         for (int g = 0; g < SIDES; g++) {
-            const float scale = half_bits_to_float((uint16_t)(scale_of[g][i / 2] >> (16 * (i % 2))));
+            const float scale = int4_scale((uint16_t)(scale_of[g][i / 2] >> (16 * (i % 2))));
 #pragma unroll
             for (int t = 0; t < TILES; t++)
 #pragma unroll
@@ -168,11 +168,10 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 {
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr int TOKENS = 16, LD = kInt4BlockCols + 8;  // (16 lanes' reads, a token each, meet no bank twice)
-    constexpr int X_BYTES = TOKENS * LD * 2, WAVE_BYTES = X_BYTES + 4 * PER_BLOCK * TOKENS;
+    constexpr int WAVE_BYTES = TOKENS * LD * 2;
     const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n16 = lane & 15, quarter = lane >> 4, from_lane = 4 * (4 * n16 + quarter);
     uint16_t *s_x = reinterpret_cast<uint16_t *>(smem + part * WAVE_BYTES);
-    float *s_sum = reinterpret_cast<float *>(smem + part * WAVE_BYTES + X_BYTES);
     f32x4 *joined = reinterpret_cast<f32x4 *>(smem);
     const bool gated = int4_gates(a);
     const int row_tiles = (a.rows + 15) / 16;
@@ -215,8 +214,6 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
             for (int j = 0; j < 4; j++) {
                 if (4 * j >= it.ntok) continue;
                 *reinterpret_cast<u32x4 *>(&s_x[(4 * j + quarter) * LD + 8 * n16]) = x_next[j];
-                const float all = int4_group_sum<PER_BLOCK>(x_next[j]);
-                if ((n16 + 1) % (16 / PER_BLOCK) == 0) s_sum[(n16 * PER_BLOCK / 16) * TOKENS + 4 * j + quarter] = all;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -239,8 +236,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
                 rows.load(w_next, b + 1, b1 - 1);
                 load_x(b + 1);
             }
-            int4_block<SIDES, 1, PER_BLOCK, 1, TOKENS>(acc, w, 0, scale_of, zero_of, bool(m.zero), s_x + n16 * LD + 8 * quarter, LD,
-                                                           s_sum + 4 * quarter);
+            int4_block<SIDES, 1, PER_BLOCK, 1>(acc, w, 0, scale_of, zero_of, bool(m.zero), s_x + n16 * LD + 8 * quarter, LD);
         }
         __syncthreads();  // all have read their activations: the sums take their place
 #pragma unroll
@@ -275,7 +271,6 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int
     constexpr int AT_ONCE = TILES == 1 ? 32 : 16, LD_SCALE = AT_ONCE + 8, LD_ZERO = AT_ONCE + 8;
     using Rows = Int4Rows<2, BLOCKS, PER_BLOCK>;
     __shared__ __align__(16) uint16_t s_x[2][TOKENS * LD];
-    __shared__ __align__(16) float s_sum[2][BLOCKS * PER_BLOCK * TOKENS];
     __shared__ __align__(16) uint16_t s_scale[4][2 * 16 * LD_SCALE];
     __shared__ __align__(16) uint8_t s_zero[4][2 * 16 * LD_ZERO];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -337,7 +332,7 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int
 #pragma unroll
             for (int t = 0; t < TILES; t++) acc[g][t] = (f32x4){0, 0, 0, 0};
         __syncthreads();  // the unit before has read its last steps
-        const int x_at = (place + (alone ? n16 & 3 : n16)) * LD + 8 * quarter, sum_at = alone ? place : 4 * quarter;
+        const int x_at = (place + (alone ? n16 & 3 : n16)) * LD + 8 * quarter;
         const int last_step = (a.blocks - 1) / BLOCKS * BLOCKS;
         auto one_step = [&](int b, int g_from, int turn) {
             if (kInt4BlockCols * b + COLS > a.cols) {
@@ -349,8 +344,6 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int
                 if (alone && j > 1) break;
                 const int token = place + stagers * j + stager;
                 *reinterpret_cast<u32x4 *>(&s_x[turn][token * LD + 8 * piece]) = x_next[j];
-                const float all = int4_group_sum<PER_BLOCK>(x_next[j]);
-                if ((piece + 1) % (16 / PER_BLOCK) == 0) s_sum[turn][(piece * PER_BLOCK / 16) * TOKENS + token] = all;
             }
             if (alone) {
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -385,8 +378,7 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int
 #pragma unroll
             for (int u = 0; u < BLOCKS; u++) {
                 if (b + u >= a.blocks) break;
-                int4_block<2, TILES, PER_BLOCK, BLOCKS, TOKENS>(acc, w[u], u, scale_of, zero_of, true, s_x[turn] + x_at + kInt4BlockCols * u, LD,
-                                                                s_sum[turn] + u * PER_BLOCK * TOKENS + sum_at);
+                int4_block<2, TILES, PER_BLOCK, BLOCKS>(acc, w[u], u, scale_of, zero_of, true, s_x[turn] + x_at + kInt4BlockCols * u, LD);
             }
         };
         const int span = a.blocks_per_group > 1 ? AT_ONCE * a.blocks_per_group : AT_ONCE / PER_BLOCK;  // blocks whose scales lie in LDS
@@ -423,7 +415,7 @@ void fill_shape(Int4Args *a, int rows, int cols, int group)
 template <int SIDES, int PER_BLOCK>
 qmoe_status launch_split_variant(const Int4Args &a, int grid, hipStream_t s)
 {
-    const size_t x = a.split * (16 * (kInt4BlockCols + 8) * 2 + 4 * PER_BLOCK * 16);
+    const size_t x = a.split * (16 * (kInt4BlockCols + 8) * 2);
     const size_t smem = std::max(x, (size_t)a.split * SIDES * 64 * sizeof(f32x4));
     const qmoe_status st = allow_lds(k_int4_split<SIDES, PER_BLOCK>, smem);
     if (st != QMOE_OK) return st;

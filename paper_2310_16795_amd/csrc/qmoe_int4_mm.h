@@ -9,10 +9,9 @@ namespace {
 // A workgroup of four wavefronts multiplies 256 rows (gated: 128 of each projection) with 64 tokens, 128 columns a step: four tiles of 16 rows
 // a wavefront, 64 matrix instructions a step.
 // The activations go through LDS in two turns and are read by all four; a wavefront's weights are its alone: loaded 64 bytes a row,
-// brought to their lanes by ds_bpermute and decoded (int4_plus16) 32 columns at a time, right before the 16 matrix instructions that use
+// brought to their lanes by ds_bpermute and decoded (int4_weights) 32 columns at a time, right before the 16 matrix instructions that use
 // them, so that decoding one tile runs beside multiplying the one before and few registers hold operands.  Two wavefronts a SIMD: the
 // sums (64 registers) are scaled into the result (64) in fp32, which accumulation registers could not take part in.
-// With PER_BLOCK groups of 128 / PER_BLOCK columns, a group's sum starts at -(16 + z) * sum of x (formed by those who stage x).
 // Scales and zero points of kMmAtOnce groups lie in LDS, a wavefront's own.
 // 12288 x 2080 (gated, groups of 128), 4001 tokens: 263 us, 780 TFLOP/s; the matrix cores are busy for 86 us of it, vector instructions (decoding 34 %,
 // scaling 15, group sums and epilogue the rest) for 137, and the two overlap in part.  The library's bf16 product of that shape is 196 us, without the activation.
@@ -26,7 +25,6 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
     constexpr int TOKENS = 16 * kMmTiles, OUT_TILES = GATED ? kMmRows / 2 : kMmRows, LD = kInt4BlockCols + 8;
     constexpr int LD_SCALE = kMmAtOnce + 8, LD_ZERO = kMmAtOnce + 8;
     __shared__ __align__(16) uint16_t s_x[2][TOKENS * LD];
-    __shared__ __align__(16) float s_sum[2][PER_BLOCK * TOKENS];
     __shared__ __align__(16) uint16_t s_scale[4][16 * kMmRows * LD_SCALE];
     __shared__ __align__(16) uint8_t s_zero[4][ZEROS ? 16 * kMmRows * LD_ZERO : 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -72,8 +70,6 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
             for (int t = 0; t < kMmTiles; t++) {
                 const int token = 16 * t + stager;
                 *reinterpret_cast<u32x4 *>(&s_x[buf][token * LD + 8 * piece]) = x_next[t];
-                const float s = int4_group_sum<PER_BLOCK>(x_next[t]);
-                if ((piece + 1) % (16 / PER_BLOCK) == 0) s_sum[buf][(piece * PER_BLOCK / 16) * TOKENS + token] = ZEROS ? s : -24.0f * s;
             }
         };
         // groups g0 .. g0 + kMmAtOnce - 1 of the wavefront's 64 rows: four lanes a row, eight groups a lane
@@ -127,6 +123,7 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
                 load(min(blk + 1, a.blocks - 1));
                 const int g_at = (a.blocks_per_group > 1 ? blk / a.blocks_per_group : blk * PER_BLOCK) - g_from;
                 f32x4 sum[kMmRows][kMmTiles];
+                Int4Zero zero[kMmRows];
 #pragma unroll
                 for (int s = 0; s < 4; s++) {
                     const int g = s * PER_BLOCK / 4;
@@ -136,25 +133,22 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
                     for (int t = 0; t < kMmTiles; t++) xf[t] = *reinterpret_cast<const bf16x8 *>(&s_x[buf][x_at + 16 * t * LD + 32 * s]);
                     if (s * PER_BLOCK % 4 == 0) {
 #pragma unroll
-                        for (int t = 0; t < kMmTiles; t++) {
-                            const f32x4 xs = *reinterpret_cast<const f32x4 *>(&s_sum[buf][g * TOKENS + 16 * t + 4 * quarter]);
+                        for (int r = 0; r < kMmRows; r++) {
+                            zero[r] = int4_zero(ZEROS ? s_zero[wave][(16 * r + n16) * LD_ZERO + g_at + g] : 8u);
 #pragma unroll
-                            for (int r = 0; r < kMmRows; r++) {
-                                if constexpr (ZEROS) sum[r][t] = xs * (-16.0f - (float)s_zero[wave][(16 * r + n16) * LD_ZERO + g_at + g]);
-                                else sum[r][t] = xs;
-                            }
+                            for (int t = 0; t < kMmTiles; t++) sum[r][t] = (f32x4){0, 0, 0, 0};
                         }
                     }
 #pragma unroll
                     for (int r = 0; r < kMmRows; r++) {
-                        const bf16x8 wf = int4_plus16(w[r][s]);
+                        const bf16x8 wf = int4_weights(w[r][s], zero[r]);
 #pragma unroll
                         for (int t = 0; t < kMmTiles; t++) sum[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[t], wf, sum[r][t], 0, 0, 0);
                     }
                     if ((s + 1) * PER_BLOCK % 4) continue;
 #pragma unroll
                     for (int r = 0; r < kMmRows; r++) {
-                        const float scale = half_bits_to_float(s_scale[wave][(16 * r + n16) * LD_SCALE + g_at + g]);
+                        const float scale = int4_scale(s_scale[wave][(16 * r + n16) * LD_SCALE + g_at + g]);
 #pragma unroll
                         for (int t = 0; t < kMmTiles; t++)
 #pragma unroll

@@ -1,0 +1,54 @@
+"""Edges of the operators around the layer on the GPU, against their formulas in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_16795_amd as q
+from test_gpu_operators import _matrix, _near, _out, _untouched, _up, _weights, gpu  # noqa: F401
+
+import plain
+import plain_exact
+
+pytestmark = pytest.mark.gpu
+
+OUTLIERS = [  # rows, cols, batch, group, zeros, activation, y: little work, and tiles of 16, 32 and 64 tokens
+    (30, 300, 1, 64, True, "none", "f32"), (200, 390, 16, 128, False, "relu", "f32"), (12000, 600, 33, 32, True, "silu", "f32"), (12000, 600, 33, 256, False, "none", "bf16"),
+    (12000, 600, 300, 128, True, "none", "f32"), (12000, 600, 300, 64, False, "gelu", "f32"), (1601, 200, 3601, 128, False, "none", "f32"),
+    (1601, 200, 3601, 32, True, "none", "f32"), (3202, 330, 3590, 64, True, "silu", "f32"), (3202, 330, 3590, 128, False, "silu", "f32"),
+]
+
+
+@pytest.mark.parametrize("large", [1e4, 3e38])
+@pytest.mark.parametrize("rows,cols,batch,group,zeros,act,yt", OUTLIERS)
+def test_int4_weight_of_zero_takes_nothing_from_a_large_activation(gpu, rows, cols, batch, group, zeros, act, yt, large):  # noqa: F811
+    rng = np.random.default_rng(rows + batch)
+    values, _, s, zero = _weights(rng, rows, cols, group, zeros, False)
+    x = rng.standard_normal((batch, cols))
+    at = rng.choice(cols, 5)
+    for c in at:
+        values[:, c] = 8 if zero is None else zero[:, c // group]
+    x[np.arange(batch), at[np.arange(batch) % 5]] = large * (-1.0) ** np.arange(batch)
+    xd, x64 = _up(x, gpu, "bf16")
+    y, held = _out(batch, rows // 2 if act in ("silu", "gelu") else rows, gpu, yt)
+    W = _matrix(gpu, (values, q.qmoe_int4_pack_host(values), s, zero), cols, group)
+    q.qmoe_int4_matvec(W.desc, xd, y, activation=q.ACTIVATIONS[act])
+    want, err = plain_exact.int4_product(x64, values, s, zero, group, act)
+    _near(y, want, err, yt)
+    _untouched(held, *y.shape)
+    d = y.double().cpu().numpy() - want  # as a whole far closer than the bound on each
+    assert yt != "f32" or np.linalg.norm(d) <= 2e-6 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("rows,cols,batch", [(30, 300, 1), (12000, 600, 33), (12000, 600, 300), (1601, 200, 3601)])
+def test_int4_product_of_the_largest_activation_is_finite(gpu, rows, cols, batch):  # noqa: F811
+    """One activation near the end of bf16 times the largest weight, 15 steps of 2^-10: finite, with nothing else next to it to lose."""
+    values, zero = np.full((rows, cols), 15, dtype=np.uint8), np.zeros((rows, -(-cols // 64)), dtype=np.uint8)
+    s = np.full(zero.shape, 2.0 ** -10, dtype=np.float16).view(np.uint16)
+    x = np.zeros((batch, cols))
+    x[np.arange(batch), np.arange(batch) * 7 % cols] = 3e38
+    xd, x64 = _up(x, gpu, "bf16")
+    y = torch.empty((batch, rows), device=gpu)
+    W = _matrix(gpu, (values, q.qmoe_int4_pack_host(values), s, zero), cols, 64)
+    q.qmoe_int4_matvec(W.desc, xd, y)
+    want, err = plain_exact.int4_product(x64, values, s, zero, 64, "none")
+    _near(y, want, 0 * err, "f32")
