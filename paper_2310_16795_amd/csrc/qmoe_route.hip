@@ -87,8 +87,24 @@ __device__ __forceinline__ void finish(const RouteArgs &a, int t, int l, int min
     }
 }
 
-// exp(v - top) for a sum: the hardware's exponential, off by |v - top| roundings or so, which where it counts is a few.  top is finite.
-__device__ __forceinline__ float share(float v, float top) { return __expf(v - top); }
+// exp(v - top) for a sum; top is finite and the largest.  The hardware's exponential is that of 2^p, p = x log2 e rounded to fp32, which is off by |x| half steps or so
+// and by the same for equal logits: 2047 of them 5.7 below the largest put a sum of 2048 off by four to six (root mean square over such distances).  What p stands for, p ln 2,
+// is known to more bits than x has (ln 2 in two parts), and the difference put right.  (expf: 12.0 us for 4096 tokens of 2048, 10.4 so, 9.9 uncorrected.)
+__device__ __forceinline__ float share(float v, float top)
+{
+    const float x = fmaxf(v - top, -200.0f);  // (exp(-200) is 0)
+    const float p = x * 1.4426950408889634f;
+    const float off = fmaf(p, 1.9046542e-9f, fmaf(p, -0.6931471824645996f, x));
+    const float e = __expf(x);
+    return fmaf(e, off, e);
+}
+// The sum over N values, halves joined: log2 N roundings.
+template <int N, int PER>
+__device__ __forceinline__ float shares(const float (&v)[PER], float top, int from = 0)
+{
+    if constexpr (N == 1) return share(v[from], top);
+    else return shares<N / 2>(v, top, from) + shares<N / 2>(v, top, from + N / 2);
+}
 
 // Four consecutive logits from expert e on (n_experts a multiple of four, or elementwise).
 template <int TYPE>
@@ -163,9 +179,7 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
 #pragma unroll
             for (int i = 1; i < PER; i++) top = fmaxf(top, v[i]);
             top = fmaxf(lanes_max<LANES>(top), -FLT_MAX);
-#pragma unroll
-            for (int i = 0; i < PER; i++) sum += share(v[i], top);
-            sum = lanes_sum<LANES>(sum);
+            sum = lanes_sum<LANES>(shares<PER>(v, top));
         }
     }
     float best = key[0];
@@ -224,9 +238,7 @@ __global__ __launch_bounds__(kWideLanes) void k_route_wide(const RouteArgs a)
         __syncthreads();
         for (int w = 0; w < WAVES; w++) top = fmaxf(top, s_top[w]);
         top = fmaxf(top, -FLT_MAX);
-#pragma unroll
-        for (int i = 0; i < PER; i++) sum += share(key[i], top);
-        sum = lanes_sum<64>(sum);
+        sum = lanes_sum<64>(shares<PER>(key, top));
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
         sum = 0.0f;

@@ -52,3 +52,20 @@ def test_int4_product_of_the_largest_activation_is_finite(gpu, rows, cols, batch
     q.qmoe_int4_matvec(W.desc, xd, y)
     want, err = plain_exact.int4_product(x64, values, s, zero, 64, "none")
     _near(y, want, 0 * err, "f32")
+
+
+@pytest.mark.parametrize("e", [2048, 4096, 16384])
+def test_route_gates_over_equal_logits(gpu, e):  # noqa: F811
+    """One expert at 0 and the others all at -d, 512 values of d where they make up most of the sum: an error of exp(-d) is the same in every term and stays.
+    Done accurately the gate is off by the rounding of exp(-d), of quotient and sums (terms of one size add up exactly by halves; where the one joins, sums of
+    1/2, 1/4, ... of the whole are rounded: the root of 1 + 1/4 + ... for all of them): each evenly spread over half a step, 1/sqrt(3) of it as a root mean square,
+    together sqrt(1 + 1 + 4/3) / sqrt(3) = 1.05 half steps.  Twice that is allowed."""
+    d = np.linspace(np.log(e) - 2.0, np.log(e) - 1.4, 512).astype(np.float32)
+    l = np.repeat(-d[:, None], e, axis=1)
+    l[:, 7] = 0.0
+    idx, gate = torch.empty((512, 1), dtype=torch.int32, device=gpu), torch.empty((512, 1), device=gpu)
+    q.qmoe_route(torch.from_numpy(l).to(gpu), idx, gate)
+    want = 1.0 / (1.0 + (e - 1) * np.exp(-d.astype(np.float64)))
+    rel = (gate.cpu().numpy()[:, 0].astype(np.float64) - want) / want
+    assert (idx == 7).all()
+    assert np.sqrt((rel ** 2).mean()) <= 2 * 1.05 * plain.U32, f"{np.sqrt((rel ** 2).mean()) / plain.U32:.2f} half steps"
