@@ -55,6 +55,7 @@ class DeviceMatrix:
                                   self.scale.data_ptr() if self.scale is not None else None, rows,
                                   cols, int(codes.size), order,
                                   self.minmax.data_ptr() if self.minmax is not None else None)
+        self.desc.held = (self.codes, self.row_off, self.scale, self.minmax)  # (what is taken from here lives on its own)
 
 
 class DeviceLayer:
@@ -178,6 +179,7 @@ class DeviceNorm:
             raise ValueError("weight and bias must be float32 vectors of one width")
         self.weight, self.bias, self.d = weight, bias, given[0].numel() if given else None
         self.desc = B.qmoe_norm(self.KINDS[kind], eps, *(B._dev_ptr(t) or None for t in (weight, bias)))
+        self.desc.held = (weight, bias)
         self.ref = ctypes.byref(self.desc)
 
 
@@ -192,7 +194,7 @@ def _int4_shapes(weights: torch.Tensor, scale: torch.Tensor, zero: "torch.Tensor
 
 
 class DeviceInt4Matrix:
-    """One four-bit matrix in device memory and its qmoe_int4_matrix descriptor."""
+    """One four-bit matrix in device memory and its qmoe_int4_matrix descriptor, which keeps the tensors that it points to."""
 
     def __init__(self, weights: torch.Tensor, scale: torch.Tensor, cols: int, group: int, zero: "torch.Tensor | None" = None):
         """weights: uint8 [rows, row bytes]; scale: binary16 [rows, groups]; zero: uint8 [rows, groups] or None (= 8)."""
@@ -200,6 +202,7 @@ class DeviceInt4Matrix:
         _int4_shapes(weights, scale, zero, (rows,), cols, group)
         self.weights, self.scale, self.zero = weights, scale, zero
         self.desc = B.qmoe_int4_matrix(B._dev_ptr(weights), B._dev_ptr(scale), B._dev_ptr(zero) or None, rows, cols, group, 0)
+        self.desc.held = (weights, scale, zero)
 
 
 class DeviceInt4Layer:

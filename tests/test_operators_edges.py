@@ -1,9 +1,13 @@
-"""Edges of the operators around the layer, on the CPU: calls of the checked CPU build of the kernels (tests/operators/edge_calls.py)."""
+"""Edges of the operators around the layer, on the CPU: calls of the checked CPU build of the kernels (tests/operators/edge_calls.py), and what the
+holders of device tensors keep and refuse."""
+import gc
 import os
 import subprocess
 import sys
+import weakref
 
 import pytest
+import torch
 
 from test_operators_lanes import library  # noqa: F401
 
@@ -15,3 +19,28 @@ def test_edge_calls(library, kind, count, units):  # noqa: F811
     cmd = [sys.executable, os.path.join(HERE, "operators", "edge_calls.py"), kind, str(count)]
     r = subprocess.run(cmd, env={**os.environ, "QMOE_LIBRARY": library, "LANES_COMPUTE_UNITS": str(units)}, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600)
     assert r.returncode == 0 and r.stdout.rstrip().endswith("done"), r.stdout[-3000:]
+
+
+@pytest.fixture
+def on_the_host(monkeypatch):
+    """Descriptors of host tensors, for what does not launch anything."""
+    from paper_2310_16795_amd import _binding
+
+    monkeypatch.setattr(_binding, "_dev_ptr", lambda t: 0 if t is None else t.data_ptr())
+
+
+def test_a_descriptor_keeps_its_tensors(on_the_host):
+    """The calls take a descriptor alone: what it points to lives as long as it does."""
+    from paper_2310_16795_amd import device as dev
+
+    made = [torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((4, 2), dtype=torch.float16), torch.zeros((4, 2), dtype=torch.uint8), torch.ones(8), torch.zeros(8)]
+    alive = [weakref.ref(t) for t in made]
+    matrix, norm = dev.DeviceInt4Matrix(made[0], made[1], 128, 64, made[2]).desc, dev.DeviceNorm("layer", made[3], made[4]).desc
+    addresses = [t.data_ptr() for t in made]
+    del made
+    gc.collect()
+    assert all(r() is not None for r in alive)
+    assert [matrix.weights, matrix.scale_f16, matrix.zero, norm.weight, norm.bias] == addresses
+    del matrix, norm
+    gc.collect()
+    assert all(r() is None for r in alive)
