@@ -398,12 +398,22 @@ def _current_device() -> int:
     return device
 
 
-def _here(*tensors) -> None:
-    """A call is enqueued on the current device: its tensors must be there."""
+def _here(*tensors, descs=()) -> None:
+    """A call is enqueued on the current device: its tensors must be there, and what its descriptors point to."""
     here = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the current device is {here}")
+    for d in descs:
+        if d is not None and getattr(d, "device", here) not in (here, None):
+            raise ValueError(f"what a descriptor points to is on device {d.device}, but the current device is {here}")
+
+
+def _one_device(tensors) -> None:
+    """What one descriptor points to lies on one device."""
+    given = [t for t in tensors if t is not None]
+    if any(t.device != given[0].device for t in given):
+        raise ValueError("tensors on one device expected")
 
 
 def _matrix(t, rows: int, cols: int, what: str):
@@ -450,6 +460,10 @@ def _norm_ptr(n, d: int, what: str):
     return n.ref
 
 
+def _desc(n):
+    return n if n is None or isinstance(n, qmoe_norm) else n.desc
+
+
 def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, post=None, alpha: float = 1.0, channel_scale=None,
                        pre=None, copies: int = 1, stream=None) -> None:
     """h, h_out: device [n, d] float32 or bfloat16 (h_out may be h); y: [n * k, d] float32 or bfloat16; x: [n * copies, d] bfloat16;
@@ -461,7 +475,7 @@ def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, pos
     xp, xl = (0, 0) if x is None else _bf16_matrix(x, n * copies, d, "x")
     if ot != ht:
         raise ValueError("h_out must be of h's type")
-    _here(h, y, h_out, x, gate, channel_scale)
+    _here(h, y, h_out, x, gate, channel_scale, descs=(_desc(post), _desc(pre)))
     _check(lib().qmoe_residual_norm(hp, ht, hl, yp, yt, yl, k, _vector(gate, n * k, "gate"), _norm_ptr(post, d, "post"), alpha,
                                     _vector(channel_scale, d, "channel_scale"), _norm_ptr(pre, d, "pre"), op, ol, xp, xl, copies, n, d,
                                     _stream_ptr(stream)), "qmoe_residual_norm")
@@ -529,7 +543,7 @@ def qmoe_int4_matvec(W: qmoe_int4_matrix, x_bf16, y, activation: int = ACT_NONE,
     batch, rows = x_bf16.shape[0], W.rows
     xp, xl = _bf16_matrix(x_bf16, batch, W.cols, "x")
     yp, yt, yl = _matrix(y, batch, rows // 2 if activation >= ACT_SILU_GATED else rows, "y")
-    _here(x_bf16, y)
+    _here(x_bf16, y, descs=(W,))
     _check(lib().qmoe_int4_matvec(byref(W), xp, xl, batch, activation, yp, yt, yl, _stream_ptr(stream)), "qmoe_int4_matvec")
 
 

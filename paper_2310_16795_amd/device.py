@@ -177,9 +177,10 @@ class DeviceNorm:
         given = [t for t in (weight, bias) if t is not None]
         if any(t.dtype != torch.float32 or t.dim() != 1 or t.numel() != given[0].numel() for t in given):
             raise ValueError("weight and bias must be float32 vectors of one width")
+        B._one_device(given)
         self.weight, self.bias, self.d = weight, bias, given[0].numel() if given else None
         self.desc = B.qmoe_norm(self.KINDS[kind], eps, *(B._dev_ptr(t) or None for t in (weight, bias)))
-        self.desc.held = (weight, bias)
+        self.desc.held, self.desc.device = (weight, bias), given[0].get_device() if given else None
         self.ref = ctypes.byref(self.desc)
 
 
@@ -191,6 +192,7 @@ def _int4_shapes(weights: torch.Tensor, scale: torch.Tensor, zero: "torch.Tensor
         raise ValueError("scale must be 16-bit [..., rows, groups]")
     if zero is not None and (zero.dtype != torch.uint8 or zero.shape != scale.shape):
         raise ValueError("zero must be uint8 [..., rows, groups]")
+    B._one_device([weights, scale, zero])
 
 
 class DeviceInt4Matrix:
@@ -202,7 +204,7 @@ class DeviceInt4Matrix:
         _int4_shapes(weights, scale, zero, (rows,), cols, group)
         self.weights, self.scale, self.zero = weights, scale, zero
         self.desc = B.qmoe_int4_matrix(B._dev_ptr(weights), B._dev_ptr(scale), B._dev_ptr(zero) or None, rows, cols, group, 0)
-        self.desc.held = (weights, scale, zero)
+        self.desc.held, self.desc.device = (weights, scale, zero), weights.get_device()
 
 
 class DeviceInt4Layer:
@@ -214,6 +216,7 @@ class DeviceInt4Layer:
         self.n_experts, self.d_model, self.d_ff, self.group = wi[0].shape[0], d_model, d_ff, group
         self.activation = B.ACTIVATIONS[activation]
         self.device = wi[0].device
+        B._one_device([wi[0], wo[0]])
         self.tensors, self.desc_dev = (tuple(wi), tuple(wo)), []
         rows_wi = d_ff if self.activation == B.ACT_RELU else 2 * d_ff
         for (w, s, z), rows, cols in ((wi, rows_wi, d_model), (wo, d_model, d_ff)):

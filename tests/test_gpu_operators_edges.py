@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2310_16795_amd as q
+from paper_2310_16795_amd import device as dev
 from test_gpu_operators import _matrix, _near, _out, _untouched, _up, _weights, gpu  # noqa: F401
 
 import plain
@@ -69,3 +70,19 @@ def test_route_gates_over_equal_logits(gpu, e):  # noqa: F811
     rel = (gate.cpu().numpy()[:, 0].astype(np.float64) - want) / want
     assert (idx == 7).all()
     assert np.sqrt((rel ** 2).mean()) <= 2 * 1.05 * plain.U32, f"{np.sqrt((rel ** 2).mean()) / plain.U32:.2f} half steps"
+
+
+def test_descriptors_of_another_device_are_refused(gpu):  # noqa: F811
+    """(With one GPU another is a number that the descriptors say they are on.)"""
+    x, y = torch.zeros((2, 64), dtype=torch.bfloat16, device=gpu), torch.zeros((2, 32), device=gpu)
+    W = _matrix(gpu, _weights(np.random.default_rng(0), 32, 64, 32, False, True), 64, 32)
+    h, norm = torch.zeros((2, 64), device=gpu), dev.DeviceNorm("rms", torch.ones(64, device=gpu))
+    assert W.desc.device == norm.desc.device == x.get_device() and dev.DeviceNorm("rms").desc.device is None
+    calls = [lambda: q.qmoe_int4_matvec(W.desc, x, y), lambda: q.qmoe_residual_norm(h, x=x, pre=norm), lambda: q.qmoe_residual_norm(h, x=x, pre=norm.desc),
+             lambda: q.qmoe_residual_norm(h, h, torch.empty_like(h), post=norm)]
+    for call in calls:
+        call()
+    W.desc.device = norm.desc.device = x.get_device() + 1
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()

@@ -44,3 +44,21 @@ def test_a_descriptor_keeps_its_tensors(on_the_host):
     del matrix, norm
     gc.collect()
     assert all(r() is None for r in alive)
+
+
+def test_what_a_descriptor_points_to_is_on_one_device(on_the_host):
+    from paper_2310_16795_amd import device as dev
+
+    host = dict(w=torch.zeros((4, 64), dtype=torch.uint8), s=torch.zeros((4, 2), dtype=torch.float16), z=torch.zeros((4, 2), dtype=torch.uint8))
+    for name in host:
+        t = {**host, name: host[name].to("meta")}
+        with pytest.raises(ValueError, match="one device"):
+            dev.DeviceInt4Matrix(t["w"], t["s"], 128, 64, t["z"])
+        t = {k: v.view(1, 4, -1) for k, v in t.items()}
+        with pytest.raises(ValueError, match="one device"):
+            dev.DeviceInt4Layer(tuple(t.values()), tuple(t.values()), 128, 4, 64)
+    layer = [tuple(v.view(1, 4, -1) for v in host.values()), (torch.zeros((1, 128, 64), dtype=torch.uint8, device="meta"), torch.zeros((1, 128, 1), dtype=torch.float16, device="meta"), None)]
+    with pytest.raises(ValueError, match="one device"):
+        dev.DeviceInt4Layer(*layer, 128, 4, 64)
+    with pytest.raises(ValueError, match="one device"):
+        dev.DeviceNorm("layer", torch.ones(8), torch.zeros(8, device="meta"))
