@@ -184,14 +184,20 @@ class DeviceNorm:
         self.ref = ctypes.byref(self.desc)
 
 
+def _binary16() -> tuple:
+    return tuple(getattr(torch, name) for name in ("float16", "int16", "uint16") if hasattr(torch, name))
+
+
 def _int4_shapes(weights: torch.Tensor, scale: torch.Tensor, zero: "torch.Tensor | None", lead: tuple, cols: int, group: int):
     groups = (cols + group - 1) // group
     if weights.dtype != torch.uint8 or tuple(weights.shape) != (*lead, B.qmoe_int4_row_bytes(cols)):
         raise ValueError("weights must be uint8 [..., rows, row bytes]")
-    if scale.element_size() != 2 or tuple(scale.shape) != (*lead, groups):
-        raise ValueError("scale must be 16-bit [..., rows, groups]")
+    if scale.dtype not in _binary16() or tuple(scale.shape) != (*lead, groups):
+        raise ValueError("scale must be binary16 (or 16-bit integers, its bits) [..., rows, groups]")
     if zero is not None and (zero.dtype != torch.uint8 or zero.shape != scale.shape):
         raise ValueError("zero must be uint8 [..., rows, groups]")
+    if weights.data_ptr() % 16:
+        raise ValueError("weights must be 16-byte aligned")
     B._one_device([weights, scale, zero])
 
 

@@ -62,3 +62,23 @@ def test_what_a_descriptor_points_to_is_on_one_device(on_the_host):
         dev.DeviceInt4Layer(*layer, 128, 4, 64)
     with pytest.raises(ValueError, match="one device"):
         dev.DeviceNorm("layer", torch.ones(8), torch.zeros(8, device="meta"))
+
+
+def test_scales_are_binary16_and_weights_aligned(on_the_host):
+    """A scale of another 16-bit type would be read as binary16; a layer's descriptors are not seen by the call, so what they point to is checked here."""
+    from paper_2310_16795_amd import device as dev
+
+    w, s = torch.zeros((2, 128, 64), dtype=torch.uint8), torch.ones((2, 128, 2), dtype=torch.float16)
+    odd = torch.zeros(w.numel() + 8, dtype=torch.uint8)[8:].view(w.shape)
+    for kind in (torch.float16, torch.int16, torch.uint16):
+        dev.DeviceInt4Matrix(w[0], s[0].view(kind), 128, 64)
+        dev.DeviceInt4Layer((w, s.view(kind), None), (w, s.view(kind), None), 128, 128, 64)
+    for kind in (torch.bfloat16, torch.float32, torch.uint8):
+        with pytest.raises(ValueError, match="binary16"):
+            dev.DeviceInt4Matrix(w[0], s[0].to(kind), 128, 64)
+        with pytest.raises(ValueError, match="binary16"):
+            dev.DeviceInt4Layer((w, s, None), (w, s.to(kind), None), 128, 128, 64)
+    with pytest.raises(ValueError, match="aligned"):
+        dev.DeviceInt4Matrix(odd[0], s[0], 128, 64)
+    with pytest.raises(ValueError, match="aligned"):
+        dev.DeviceInt4Layer((w, s, None), (odd, s, None), 128, 128, 64)
