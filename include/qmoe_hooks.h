@@ -45,6 +45,15 @@ int qmoe_hook_several_lanes(const qmoe_dict *d, int format, int n_experts, int d
  */
 qmoe_status qmoe_hook_rows_shares(int rows, const int items[3], int tiles_at_once, int groups, int *out);
 
+/*
+ * The kernel that a four-bit product takes on a GPU of so many compute units, computed on the host (no GPU needed): 1 k_int4_split,
+ * 2 / 3 k_int4_tile with 16 / 32 tokens, 4 k_int4_mm; 0 if the sizes are none.  rows: of the matrix.  The second one: kernels[0] and kernels[1],
+ * a layer call's two products.
+ */
+int qmoe_hook_int4_kernel(int rows, int cols, int group, int activation, int batch, int compute_units);
+qmoe_status qmoe_hook_int4_layer_kernels(int group, int activation, int n_experts, int d_model, int d_ff, int n_tokens, int compute_units,
+                                         int kernels[2]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,6 +10,7 @@ from ._binding import (  # noqa: F401
     qmoe_codes_to_device_order, qmoe_decompress, qmoe_encode_device, qmoe_dict_device_bytes, qmoe_dict_device_order, qmoe_dict_from_words, qmoe_dict_max_nonzeros, qmoe_dict_upload, qmoe_dict_words,
     qmoe_encode_host, qmoe_moe_dispatch, qmoe_moe_layer_forward, qmoe_moe_layer_workspace,
     qmoe_moe_layer_ws_layout, qmoe_set_tuning, qmoe_stream_copy, qmoe_validate_host, qmoe_hook_set, qmoe_hook_several_lanes, qmoe_hook_rows_shares,
+    qmoe_hook_int4_kernel, qmoe_hook_int4_layer_kernels,
     qmoe_moe_layer_forward_static, qmoe_static_workspace_bytes, qmoe_lane_layout_build, qmoe_lane_layout_unpack,
     qmoe_plan_lanes, qmoe_plan_row_layout, format_lanes,
     ACTIVATIONS, ACT_GELU_GATED, ACT_NONE, ACT_RELU, ACT_SILU_GATED, BF16, F32, GATES_ALL, GATES_CHOSEN, NORM_LAYER, NORM_RMS,

@@ -76,7 +76,7 @@ EXPORTS = [
     "qmoe_lane_layout_size", "qmoe_lane_layout_build", "qmoe_lane_layout_unpack", "qmoe_plan_lanes",
     "qmoe_plan_row_layout", "qmoe_hook_several_lanes", "qmoe_hook_rows_shares",
     "qmoe_residual_norm", "qmoe_route", "qmoe_int4_row_bytes", "qmoe_int4_pack_host", "qmoe_int4_unpack_host",
-    "qmoe_int4_quantize_host", "qmoe_int4_matvec", "qmoe_int4_layer_forward",
+    "qmoe_int4_quantize_host", "qmoe_int4_matvec", "qmoe_int4_layer_forward", "qmoe_hook_int4_kernel", "qmoe_hook_int4_layer_kernels",
 ]
 
 
@@ -137,6 +137,7 @@ def lib():
             "qmoe_int4_quantize_host": [vp, i, i, i, vp, vp, vp],
             "qmoe_int4_matvec": [vp, vp, sz, i, i, vp, i, sz, vp],
             "qmoe_int4_layer_forward": [vp, vp, i, i, i, i, i, vp, vp, vp, i, vp, i, vp, sz, vp],
+            "qmoe_hook_int4_kernel": [i, i, i, i, i, i], "qmoe_hook_int4_layer_kernels": [i, i, i, i, i, i, i, vp],
         }
         for name, args in operators.items():  # (a library that QMOE_LIBRARY names may be built without their units)
             if hasattr(L, name):
@@ -629,3 +630,19 @@ def qmoe_stream_copy(dst, src, stream=None) -> None:
     if dst.numel() * dst.element_size() < n:
         raise ValueError("destination too small")
     _check(lib().qmoe_stream_copy(_dev_ptr(dst), _dev_ptr(src), n, _stream_ptr(stream)), "qmoe_stream_copy")
+
+
+INT4_KERNELS = {1: "split", 2: "tile 16", 3: "tile 32", 4: "mm"}
+
+
+def qmoe_hook_int4_kernel(rows: int, cols: int, group: int, activation: int, batch: int, compute_units: int = 256) -> str:
+    """Which kernel a four-bit product takes (include/qmoe_hooks.h)."""
+    return INT4_KERNELS[lib().qmoe_hook_int4_kernel(rows, cols, group, activation, batch, compute_units)]
+
+
+def qmoe_hook_int4_layer_kernels(group: int, activation: int, n_experts: int, d_model: int, d_ff: int, n_tokens: int, compute_units: int = 256):
+    """Which kernels the two products of a four-bit layer call take (include/qmoe_hooks.h)."""
+    out = np.zeros(2, dtype=np.int32)
+    _check(lib().qmoe_hook_int4_layer_kernels(group, activation, n_experts, d_model, d_ff, n_tokens, compute_units, _host_ptr(out)),
+           "qmoe_hook_int4_layer_kernels")
+    return tuple(INT4_KERNELS[int(k)] for k in out)

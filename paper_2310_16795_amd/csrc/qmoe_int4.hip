@@ -1,5 +1,6 @@
 // Four-bit weights: the product for few tokens, and the C entry points.
 #include "qmoe_int4.h"
+#include "qmoe_hooks.h"
 
 namespace qmoe {
 namespace {
@@ -447,9 +448,10 @@ qmoe_status launch_tile(const Int4Args &a, int grid, hipStream_t s)
 // 16 13 / 15 / 17, 64 27 / 19 / 18, 256 80 / 42 / 32; 1024 x 768, 256 7.3 / 9.0 / 10, 1024 14 / 11 / 11.
 struct Int4Way {
     double us;
-    int split;  // wavefronts that share a tile's columns (k_int4_split); 0: k_int4_tile
-    int tiles;  // of 16 tokens, an item
+    int split;  // wavefronts that share a tile's columns (k_int4_split); 0: k_int4_tile, or ...
+    int tiles;  // of 16 tokens, an item (0: k_int4_mm)
 };
+int kernel_of(const Int4Way &w) { return w.split ? 1 : w.tiles ? 1 + w.tiles : 4; }
 // items: of up to 16 tokens, how many the call has at most
 Int4Way split_way(const Int4Args &a, long long items, int tokens, int cus)
 {
@@ -492,18 +494,40 @@ qmoe_status launch_way(Int4Args a, const Int4Way &way, long long items, int cus,
 // One matrix: the kernel for many tokens where it fills the GPU one and a half times (12288 x 2080, 256 tokens 39 us, the other way 32; 512 53 /
 // 56; 1024 84 / 103).  In layer calls, where tiles are partly empty, it lost (16 experts of 1024 x 4096, 4001 tokens 213, the other way 182;
 // 64 of 1024 x 2048, 1000 tokens 122 / 68).
+long long mm_units(const Int4Args &a)
+{
+    const int rows = int4_is_gated(a.activation) ? 128 : 256;
+    return ((a.batch + 63LL) / 64) * ((a.rows + rows - 1) / rows);
+}
+Int4Way matrix_way(const Int4Args &a, int cus)
+{
+    if (a.batch > 64 && 2 * mm_units(a) >= 3LL * cus && a.cols >= 8) return {0, 0, 0};
+    const Int4Way narrow = narrow_way(a, (a.batch + 15) / 16, a.batch, cus), wide = tile_way(a, 2, (a.batch + 31) / 32, cus);
+    return a.batch > 16 && a.cols >= 8 && wide.us < narrow.us ? wide : narrow;
+}
 qmoe_status launch_matrix(const Int4Args &a, int cus, hipStream_t s)
 {
-    const bool gated = int4_is_gated(a.activation);
-    const long long units = ((a.batch + 63LL) / 64) * ((a.rows + (gated ? 127 : 255)) / (gated ? 128 : 256));
-    if (a.batch > 64 && 2 * units >= 3LL * cus && a.cols >= 8) {
-        const int grid = (int)std::min<long long>(units, 64LL * cus);
-        if (gated) return a.zero ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
-        return a.zero ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
-    }
-    const long long items = (a.batch + 15) / 16, wide_items = (a.batch + 31) / 32;
-    const Int4Way narrow = narrow_way(a, items, a.batch, cus), wide = tile_way(a, 2, wide_items, cus);
-    return a.batch > 16 && a.cols >= 8 && wide.us < narrow.us ? launch_way(a, wide, wide_items, cus, s) : launch_way(a, narrow, items, cus, s);
+    const Int4Way way = matrix_way(a, cus);
+    if (way.tiles) return launch_way(a, way, (a.batch + 16LL * way.tiles - 1) / (16 * way.tiles), cus, s);
+    const int grid = (int)std::min<long long>(mm_units(a), 64LL * cus);
+    if (int4_is_gated(a.activation)) return a.zero ? launch_int4_mm_gated_zeros(a, grid, s) : launch_int4_mm_gated(a, grid, s);
+    return a.zero ? launch_int4_mm_zeros(a, grid, s) : launch_int4_mm_plain(a, grid, s);
+}
+
+// A layer call's two products.  Experts' tokens go in tiles of 16 or of 32, whichever has less to do if every expert leaves a tile partly empty.  (16 / 32, us:
+// 128 experts of 768 x 3072, 4001 tokens 209 / 175; 16 of 1024 x 4096, 4001 218 / 182; 64 of 1024 x 2048, 1000 Zipf 68 / 73; 32 of 512 x 1024, 400 28 / 31; 256 of
+// 2080 x 6144, 300 318 / 376.)
+struct Int4LayerWays {
+    Int4Way up, down;
+    long long items;
+};
+Int4LayerWays layer_ways(const Int4Args &up, const Int4Args &down, int n_experts, int n_tokens, int cus)
+{
+    const int most = up.direct ? 1 : 16;
+    const long long items = up.direct ? n_tokens : std::min(n_tokens, n_experts + n_tokens / 16), wide_items = std::min(n_tokens, n_experts + n_tokens / 32);
+    const Int4LayerWays narrow{narrow_way(up, items, most, cus), narrow_way(down, items, most, cus), items};
+    const Int4LayerWays wide{tile_way(up, 2, wide_items, cus), tile_way(down, 2, wide_items, cus), wide_items};
+    return n_tokens > 16 && wide.up.us + wide.down.us < narrow.up.us + narrow.down.us ? wide : narrow;
 }
 
 }  // namespace
@@ -562,35 +586,27 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     up.activation = activation;
     fill_shape(&up, d_ff, d_model, group);
     fill_shape(&down, d_model, d_ff, group);
-    // Experts' tokens in tiles of 16 or of 32, whichever has less to do if every expert leaves a tile partly empty.  (16 / 32, us: 128 experts of 768 x
-    // 3072, 4001 tokens 209 / 175; 16 of 1024 x 4096, 4001 218 / 182; 64 of 1024 x 2048, 1000 Zipf 68 / 73; 32 of 512 x 1024, 400 28 / 31; 256 of
-    // 2080 x 6144, 300 318 / 376.)
     up.direct = down.direct = direct ? expert_idx : nullptr;
-    long long items = direct ? n_tokens : std::min(n_tokens, n_experts + n_tokens / 16);
-    const int most = direct ? 1 : 16;
-    Int4Way up_way = narrow_way(up, items, most, di.cus), down_way = narrow_way(down, items, most, di.cus);
-    const long long wide_items = std::min(n_tokens, n_experts + n_tokens / 32);
-    const Int4Way up_wide = tile_way(up, 2, wide_items, di.cus), down_wide = tile_way(down, 2, wide_items, di.cus);
-    if (n_tokens > 16 && up_wide.us + down_wide.us < up_way.us + down_way.us) up_way = up_wide, down_way = down_wide, items = wide_items;
+    const Int4LayerWays ways = layer_ways(up, down, n_experts, n_tokens, di.cus);
     GroupedTokens g{};
     if (direct) {
         qmoe_ws_layout l;
         if ((st = qmoe_moe_layer_ws_layout(n_experts, d_model, d_ff, n_tokens, &l)) != QMOE_OK) return st;
         g.hidden = reinterpret_cast<uint16_t *>(static_cast<unsigned char *>(workspace) + l.hidden);
-    } else if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, 16 * up_way.tiles, workspace, static_cast<float *>(y),
+    } else if ((st = group_by_expert(expert_idx, n_tokens, n_experts, d_model, d_ff, 16 * ways.up.tiles, workspace, static_cast<float *>(y),
                                      y_type == QMOE_F32 ? d_model : d_model / 2, s, &g)) != QMOE_OK) {
         return st;
     }
     up.perm = down.perm = g.perm;
     up.items = down.items = g.items;
     up.n_items_dev = down.n_items_dev = g.n_items;
-    up.max_items = down.max_items = (int)items;
+    up.max_items = down.max_items = (int)ways.items;
     up.x = x_bf16;
     up.ld_x = d_model;
     up.out = g.hidden;
     up.ld_out = d_ff;
     up.out_by_slot = 1;
-    if ((st = launch_way(up, up_way, items, di.cus, s)) != QMOE_OK) return st;
+    if ((st = launch_way(up, ways.up, ways.items, di.cus, s)) != QMOE_OK) return st;
     down.x = g.hidden;
     down.ld_x = d_ff;
     down.x_by_slot = 1;
@@ -599,7 +615,33 @@ qmoe_status qmoe_int4_layer_forward(const qmoe_int4_matrix *wi, const qmoe_int4_
     down.out_f32 = y_type == QMOE_F32;
     down.gate = gate;
     down.activation = QMOE_ACT_NONE;
-    return launch_way(down, down_way, items, di.cus, s);
+    return launch_way(down, ways.down, ways.items, di.cus, s);
+}
+
+int qmoe_hook_int4_kernel(int rows, int cols, int group, int activation, int batch, int compute_units)
+{
+    if (rows < 1 || cols < 1 || batch < 1 || compute_units < 1 || !group_ok(group)) return 0;
+    Int4Args a{};
+    a.batch = batch;
+    a.activation = activation;
+    fill_shape(&a, int4_is_gated(activation) ? rows / 2 : rows, cols, group);
+    return kernel_of(matrix_way(a, compute_units));
+}
+
+qmoe_status qmoe_hook_int4_layer_kernels(int group, int activation, int n_experts, int d_model, int d_ff, int n_tokens, int compute_units,
+                                         int kernels[2])
+{
+    if (n_experts < 1 || d_model < 1 || d_ff < 1 || n_tokens < 1 || compute_units < 1 || !group_ok(group) || !kernels) return QMOE_E_INVALID_ARG;
+    static const int32_t some = 0;
+    Int4Args up{}, down{};
+    up.activation = activation;
+    fill_shape(&up, d_ff, d_model, group);
+    fill_shape(&down, d_model, d_ff, group);
+    up.direct = down.direct = n_tokens <= kInt4Direct ? &some : nullptr;
+    const Int4LayerWays ways = layer_ways(up, down, n_experts, n_tokens, compute_units);
+    kernels[0] = kernel_of(ways.up);
+    kernels[1] = kernel_of(ways.down);
+    return QMOE_OK;
 }
 
 }  // extern "C"

@@ -1,5 +1,6 @@
 """More calls of the operators on their CPU build: `python edge_calls.py KIND COUNT`, as operator_calls.py does."""
 import ctypes
+import os
 import sys
 
 import numpy as np
@@ -33,12 +34,54 @@ def outlier(rng, i):
     return st == 0 and calls.near(calls.read_rows(y_at, batch, results, results, q.F32)[0], want, err, q.F32, "y")
 
 
+UNITS = int(os.environ.get("LANES_COMPUTE_UNITS", "256"))
+
+
+def wide(rng, i):
+    """More groups than a kernel holds at a time."""
+    batch = [33, 40, 70, 130][i % 4]
+    act, group = ["none", "silu"][i // 4 % 2], [32, 128][i // 8 % 2]
+    rows, cols = 2 * int(rng.integers(100, 140)), int(rng.integers(33, 37)) * group
+    print(f"wide {i}: {q.qmoe_hook_int4_kernel(rows, cols, group, q.ACTIVATIONS[act], batch, UNITS)}", flush=True)
+    return one_product(rng, calls.Memory(i % 2), rows, cols, batch, group, i % 3 > 0, act)
+
+
+def one_product(rng, m, rows, cols, batch, group, zeros, act):
+    values, packed, s, zero = calls.weights(rng, rows, cols, group, zeros, False)
+    x_at, x = m.rows(rng.standard_normal((batch, cols)), cols, q.BF16)
+    results = rows // 2 if act == "silu" else rows
+    y_at = m.new(4 * batch * results)
+    W = q.qmoe_int4_matrix(m.put(packed, 16), m.put(s), m.put(zero), rows, cols, group, 0)
+    st = L.qmoe_int4_matvec(ctypes.byref(W), x_at, cols, batch, q.ACTIVATIONS[act], y_at, q.F32, results, None)
+    want, err = plain_exact.int4_product(x, values, s, zero, group, act)
+    return st == 0 and calls.near(calls.read_rows(y_at, batch, results, results, q.F32)[0], want, err, q.F32, "y")
+
+
+class _Groups:
+    """A generator whose draws of a layer's group are of several blocks."""
+
+    def __init__(self, rng, group):
+        self.rng, self.group = rng, group
+
+    def choice(self, of, *args):
+        return self.group if list(of) == [32, 64, 128] else self.rng.choice(of, *args)
+
+    def __getattr__(self, name):
+        return getattr(self.rng, name)
+
+
+def layer_groups(rng, i):
+    """Layer calls with groups of several blocks."""
+    sizes = (int(rng.choice([1, 3])), [5, 9, 40, 130][i % 4], 8 * int(rng.integers(20, 70)), 8 * int(rng.integers(20, 70)))
+    return calls.layer(_Groups(rng, [256, 384, 512, 1152][i // 4 % 4]), i, sizes)
+
+
 if __name__ == "__main__":
     kind, count = sys.argv[1], int(sys.argv[2])
     rng, ok = np.random.default_rng(7), True
     for i in range(count):
         before = L.lanes_reports()
-        right = {"outlier": outlier}[kind](rng, i)
+        right = {"outlier": outlier, "wide": wide, "layer_groups": layer_groups}[kind](rng, i)
         out = L.lanes_reports() - before
         ok &= bool(right) and out == 0
         if not right or out:

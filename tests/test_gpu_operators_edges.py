@@ -5,7 +5,7 @@ import torch
 
 import paper_2310_16795_amd as q
 from paper_2310_16795_amd import device as dev
-from test_gpu_operators import _matrix, _near, _out, _untouched, _up, _weights, gpu  # noqa: F401
+from test_gpu_operators import _check_layer, _layer, _matrix, _near, _out, _untouched, _up, _weights, gpu  # noqa: F401
 
 import plain
 import plain_exact
@@ -13,7 +13,7 @@ import plain_exact
 pytestmark = pytest.mark.gpu
 
 OUTLIERS = [  # rows, cols, batch, group, zeros, activation, y: little work, and tiles of 16, 32 and 64 tokens
-    (30, 300, 1, 64, True, "none", "f32"), (200, 390, 16, 128, False, "relu", "f32"), (12000, 600, 33, 32, True, "silu", "f32"), (12000, 600, 33, 256, False, "none", "bf16"),
+    (30, 300, 1, 64, True, "none", "f32"), (16000, 600, 30, 32, True, "silu", "f32"), (20000, 600, 33, 128, False, "none", "f32"), (200, 390, 16, 128, False, "relu", "f32"), (12000, 600, 33, 32, True, "silu", "f32"), (12000, 600, 33, 256, False, "none", "bf16"),
     (12000, 600, 300, 128, True, "none", "f32"), (12000, 600, 300, 64, False, "gelu", "f32"), (1601, 200, 3601, 128, False, "none", "f32"),
     (1601, 200, 3601, 32, True, "none", "f32"), (3202, 330, 3590, 64, True, "silu", "f32"), (3202, 330, 3590, 128, False, "silu", "f32"),
 ]
@@ -86,3 +86,80 @@ def test_descriptors_of_another_device_are_refused(gpu):  # noqa: F811
     for call in calls:
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+# ---------------------------------------------------------------- every kernel, by what the library chooses
+
+KERNELS = [  # kernel, rows, cols, batch, group, zeros, activation
+    ("split", 200, 300, 40, 64, True, "none"), ("split", 300, 4300, 20, 32, False, "silu"), ("tile 16", 16000, 600, 30, 32, True, "silu"), ("tile 16", 20000, 1100, 33, 32, False, "none"),
+    ("tile 16", 16000, 4300, 30, 128, True, "none"), ("tile 32", 12000, 600, 300, 128, True, "none"), ("tile 32", 12000, 1100, 300, 32, True, "gelu"), ("tile 32", 12000, 2300, 300, 128, False, "none"),
+    ("mm", 1601, 200, 3601, 32, True, "none"), ("mm", 1601, 1100, 3601, 32, True, "none"), ("mm", 1601, 1100, 3601, 32, False, "none"), ("mm", 1601, 2300, 3601, 64, True, "none"),
+    ("mm", 1601, 4300, 3601, 128, True, "none"), ("mm", 1601, 4300, 3601, 128, False, "none"), ("mm", 1601, 8400, 3601, 256, True, "none"), ("mm", 3202, 1100, 3590, 32, True, "silu"),
+    ("mm", 3202, 4300, 3590, 128, False, "gelu"), ("mm", 3202, 4300, 3590, 128, True, "silu"),
+]
+
+
+@pytest.mark.parametrize("kernel,rows,cols,batch,group,zeros,act", KERNELS)
+def test_int4_kernels_spoil_no_other_token_and_repeat_themselves(gpu, kernel, rows, cols, batch, group, zeros, act):  # noqa: F811
+    """Matrices of more groups than a kernel holds at a time among them; two tokens are not finite; a second call gives the same bits."""
+    assert q.qmoe_hook_int4_kernel(rows, cols, group, q.ACTIVATIONS[act], batch, torch.cuda.get_device_properties(0).multi_processor_count) == kernel
+    rng = np.random.default_rng(cols + batch)
+    w = _weights(rng, rows, cols, group, zeros, False)
+    x = rng.standard_normal((batch, cols)).astype(np.float32)
+    x[1, 5], x[batch - 1, cols - 1] = np.inf, np.nan
+    xd, x64 = _up(x, gpu, "bf16")
+    y, again = (torch.empty((batch, rows // 2 if act in ("silu", "gelu") else rows), device=gpu) for _ in range(2))
+    W = _matrix(gpu, w, cols, group)
+    for out in (y, again):
+        q.qmoe_int4_matvec(W.desc, xd, out, activation=q.ACTIVATIONS[act])
+    assert torch.equal(y.view(torch.int32), again.view(torch.int32))
+    keep = np.r_[0, 2:batch - 1]
+    want, err = plain_exact.int4_product(x64[keep], w[0], w[2], w[3], group, act)
+    _near(y[torch.from_numpy(keep).to(gpu)], want, err, "f32")
+    assert y[batch - 1].isnan().all() and not (act == "none" and y[1].isfinite().any())
+
+
+def test_int4_more_units_than_workgroups(gpu):  # noqa: F811
+    """k_int4_mm's workgroups take a second unit: 530000 tokens, whose results are compared on the GPU in 64 bits."""
+    rows, cols, batch, group = 257, 8, 530000, 32
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    assert q.qmoe_hook_int4_kernel(rows, cols, group, 0, batch, cus) == "mm" and -(-batch // 64) * 2 > 64 * cus
+    rng = np.random.default_rng(1)
+    w = _weights(rng, rows, cols, group, True, True)
+    x = torch.randint(-8, 9, (batch, cols), device=gpu).to(torch.bfloat16)
+    y = torch.full((batch + 1, rows), -77.0, device=gpu)
+    W = _matrix(gpu, w, cols, group)
+    q.qmoe_int4_matvec(W.desc, x, y[:batch])
+    matrix = torch.from_numpy(plain.int4_matrix(w[0], w[2], w[3], group)[0]).to(gpu).t().contiguous()
+    for t0 in range(0, batch, 100000):  # (whole numbers and powers of two: exact)
+        assert torch.equal(y[t0:t0 + 100000][:batch - t0].double(), x[t0:t0 + 100000].double() @ matrix)
+    assert (y[batch] == -77.0).all()
+
+
+LAYERS = [  # kernels of the two products, experts, d_model, d_ff, tokens, group, zeros, activation, y
+    (("tile 16", "tile 16"), 40, 1160, 1288, 64, 32, True, "silu", "bf16"), (("tile 16", "tile 16"), 30, 2112, 2112, 100, 64, True, "gelu", "f32"),
+    (("tile 16", "split"), 16, 1160, 3304, 40, 64, True, "silu", "f32"), (("tile 16", "tile 16"), 30, 1160, 1288, 300, 256, True, "silu", "bf16"),
+    (("tile 32", "tile 32"), 16, 1096, 2112, 700, 32, True, "gelu", "f32"), (("tile 32", "tile 32"), 20, 1160, 1288, 700, 512, True, "silu", "f32"),
+    (("split", "split"), 20, 776, 904, 90, 384, False, "relu", "bf16"), (("split", "split"), 5, 1288, 1160, 9, 1152, True, "gelu", "f32"), (("split", "split"), 3, 520, 776, 8, 256, True, "silu", "bf16"),
+]
+
+
+@pytest.mark.parametrize("kernels,E,d_model,d_ff,T,group,zeros,act,yt", LAYERS)
+def test_int4_layer_kernels(gpu, kernels, E, d_model, d_ff, T, group, zeros, act, yt):  # noqa: F811
+    """Gated experts with zero points and many groups in tiles, and groups of several blocks, in layer calls; a second call gives the same bits."""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    assert q.qmoe_hook_int4_layer_kernels(group, q.ACTIVATIONS[act], E, d_model, d_ff, T, cus) == kernels
+    rng = np.random.default_rng(E + T)
+    ex, layer = _layer(gpu, rng, E, d_model, d_ff, group, zeros, act)
+    idx = rng.integers(0, E, T).astype(np.int32)
+    idx[: T // 3], idx[T // 2] = E - 1, -1
+    gate = rng.random(T).astype(np.float32)
+    x, x64 = _up(rng.standard_normal((T, d_model)), gpu, "bf16")
+    (y, held), ws = _out(T, d_model, gpu, yt), layer.workspace(T)
+    args = torch.from_numpy(idx).to(gpu), y, ws, torch.from_numpy(gate).to(gpu)
+    layer.forward(x, *args)
+    first = y.clone()
+    _check_layer(ex, x64, idx, gate, group, act, yt, y.cpu(), ws, d_model, d_ff)
+    _untouched(held, T, d_model)
+    layer.forward(x, *args)
+    assert torch.equal(y, first)

@@ -14,7 +14,7 @@ from test_operators_lanes import library  # noqa: F401
 HERE = os.path.dirname(os.path.abspath(__file__))
 
 
-@pytest.mark.parametrize("kind,count,units", [("outlier", 32, 1), ("outlier", 16, 64)])
+@pytest.mark.parametrize("kind,count,units", [("outlier", 32, 1), ("outlier", 16, 64), ("wide", 16, 1), ("wide", 8, 6), ("layer_groups", 16, 1), ("layer_groups", 16, 8)])
 def test_edge_calls(library, kind, count, units):  # noqa: F811
     cmd = [sys.executable, os.path.join(HERE, "operators", "edge_calls.py"), kind, str(count)]
     r = subprocess.run(cmd, env={**os.environ, "QMOE_LIBRARY": library, "LANES_COMPUTE_UNITS": str(units)}, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600)
@@ -82,3 +82,17 @@ def test_scales_are_binary16_and_weights_aligned(on_the_host):
         dev.DeviceInt4Matrix(odd[0], s[0], 128, 64)
     with pytest.raises(ValueError, match="aligned"):
         dev.DeviceInt4Layer((w, s, None), (odd, s, None), 128, 128, 64)
+
+
+def test_which_kernel_a_four_bit_product_takes():
+    """The choice follows the sizes: few tokens, more, many; sizes that are none have no kernel."""
+    import paper_2310_16795_amd as q
+
+    one = lambda *a: q.qmoe_hook_int4_kernel(*a)  # noqa: E731
+    assert [one(20000, 1100, 128, 0, batch) for batch in (1, 33, 150, 4001)] == ["split", "tile 16", "tile 32", "mm"]
+    assert [one(rows, 7, 32, 0, 4001) for rows in (8, 20000)] == ["split"] * 2  # (the other kernels load eight columns)
+    L = q.lib()
+    assert [L.qmoe_hook_int4_kernel(*bad) for bad in ((0, 8, 32, 0, 1, 256), (8, 0, 32, 0, 1, 256), (8, 8, 48, 0, 1, 256), (8, 8, 32, 0, 0, 256), (8, 8, 32, 0, 1, 0))] == [0] * 5
+    assert q.qmoe_hook_int4_layer_kernels(128, q.ACT_RELU, 128, 768, 3072, 4001) == ("tile 32", "tile 32") and q.qmoe_hook_int4_layer_kernels(128, q.ACT_RELU, 128, 768, 3072, 8) == ("split", "split")
+    with pytest.raises(q.QmoeError):
+        q.qmoe_hook_int4_layer_kernels(128, q.ACT_RELU, 0, 768, 3072, 8)
