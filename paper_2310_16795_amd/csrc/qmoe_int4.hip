@@ -441,11 +441,13 @@ qmoe_status launch_tile(const Int4Args &a, int grid, hipStream_t s)
     return QMOE_OK;
 }
 
-// How a product of up to `tokens` (and no more than 512 or so of one matrix) is split, by what each way takes, us: a start, and rounds of what
-// the compute units hold at a time.  Fitted to single matrices of 384 x 1024, 1024 x 768, 4096 x 1024, 2080 x 6144, 6144 x 2080 and 12288 x 2080,
-// 1 to 1024 tokens, groups of 128.  Measured, k_int4_split / k_int4_tile with 16 tokens an item / with 32: 2080 x 6144, 16 tokens 10 / 32 / 36, 128 30 /
-// 33 / 38, 192 35 / 33 / 39, 512 90 / 55 / 53; 4096 x 1024, 64 8.1 / 9.6 / 11, 128 11 / 9.5 / 11, 512 28 / 18 / 16; 12288 x 2080, 1 8.6 / 13 / -,
-// 16 13 / 15 / 17, 64 27 / 19 / 18, 256 80 / 42 / 32; 1024 x 768, 256 7.3 / 9.0 / 10, 1024 14 / 11 / 11.
+// How a product of up to `tokens` (and no more than 512 or so of one matrix) is split, by what each way takes, us: a start, and as often as the compute
+// units are full (k_int4_split: wavefronts, which follow each other one by one), or in turns of a workgroup each (k_int4_tile), the steps.  Fitted to single matrices of
+// 384 x 1024, 1024 x 768, 4096 x 1024, 2080 x 6144, 6144 x 2080 and 12288 x 2080, 1 to 1024 tokens, groups of 128: from 9 us on the way it picks is within 8 % of the best
+// one in all but one of these 60 (2080 x 6144, 64 tokens, 14 %), and with groups of 32 and 64, zero points or gates in all but three of 45 (2080 x 6144: 64 tokens 12 and 32 %, 512 13 %).
+// Measured, the best k_int4_split / k_int4_tile with 16 tokens an item / with 32: 2080 x 6144, 16 tokens 9.0 / 35 / -, 128 23 /
+// 37 / 41, 256 39 / 52 / 43, 512 65 / 69 / 59; 4096 x 1024, 64 7.5 / 9.8 / 11, 128 9.7 / 10 / 11, 512 25 / 20 / 16; 12288 x 2080, 1 7.8 / 15 / -,
+// 16 12 / 17 / -, 64 25 / 23 / 19, 256 70 / 51 / 35; 1024 x 768, 256 6.8 / 9.6 / 10, 1024 - / 13 / 11.
 struct Int4Way {
     double us;
     int split;  // wavefronts that share a tile's columns (k_int4_split); 0: k_int4_tile, or ...
@@ -460,7 +462,7 @@ Int4Way split_way(const Int4Args &a, long long items, int tokens, int cus)
     Int4Way best{1e30, 1, 1};
     for (int split = 1; split <= kInt4MaxSplit && (split == 1 || split / 2 < a.blocks); split *= 2) {
         const double full = groups * split / (16.0 * cus);  // four wavefronts a SIMD
-        const double us = 1.5 + 0.5 * split + std::ceil(full) * (2.0 + block * (1.0 + 0.9 * std::min(1.0, full)) * ((a.blocks + split - 1) / split));
+        const double us = 1.5 + 0.5 * split + std::max(1.0, full) * (2.0 + block * (1.0 + 0.9 * std::min(1.0, full)) * ((a.blocks + split - 1) / split));
         if (us < best.us) best = {us, split, 1};
     }
     return best;
@@ -471,8 +473,8 @@ long long tile_units(const Int4Args &a, long long items)
 }
 Int4Way tile_way(const Int4Args &a, int tiles, long long items, int cus)
 {
-    const double more = std::max(0.0, (double)tile_units(a, items) / cus - 1.0), steps = (a.blocks + 1) / 2;
-    return {tiles == 1 ? 5.5 + steps * (1.08 + 0.58 * more) : 6.0 + steps * (1.3 + 0.8 * more), 0, tiles};
+    const double more = (double)((tile_units(a, items) - 1) / cus), steps = (a.blocks + 1) / 2;
+    return {tiles == 1 ? 5.0 + steps * (1.3 + 0.7 * more) : 5.6 + steps * (1.5 + 0.88 * more), 0, tiles};
 }
 // of up to 16 tokens an item
 Int4Way narrow_way(const Int4Args &a, long long items, int tokens, int cus)
@@ -515,8 +517,8 @@ qmoe_status launch_matrix(const Int4Args &a, int cus, hipStream_t s)
 }
 
 // A layer call's two products.  Experts' tokens go in tiles of 16 or of 32, whichever has less to do if every expert leaves a tile partly empty.  (16 / 32, us:
-// 128 experts of 768 x 3072, 4001 tokens 209 / 175; 16 of 1024 x 4096, 4001 218 / 182; 64 of 1024 x 2048, 1000 Zipf 68 / 73; 32 of 512 x 1024, 400 28 / 31; 256 of
-// 2080 x 6144, 300 318 / 376.)
+// 128 experts of 768 x 3072, 4001 tokens 210 / 164; 16 of 1024 x 4096, 4001 239 / 176; 64 of 1024 x 2048, 1000 Zipf 71 / 70; 32 of 512 x 1024, 400 28 / 29; 256 gated ones of
+// 2080 x 6144, zero points, 300 838 / 1051.)
 struct Int4LayerWays {
     Int4Way up, down;
     long long items;

@@ -90,6 +90,8 @@ def test_which_kernel_a_four_bit_product_takes():
 
     one = lambda *a: q.qmoe_hook_int4_kernel(*a)  # noqa: E731
     assert [one(20000, 1100, 128, 0, batch) for batch in (1, 33, 150, 4001)] == ["split", "tile 16", "tile 32", "mm"]
+    # one more workgroup than compute units is a turn of all its columns (2080 x 6144, 256 tokens: 272 workgroups 52 us, k_int4_split 39, tiles of 32 43)
+    assert one(2080, 6144, 128, 0, 256) in ("split", "tile 32")
     assert [one(rows, 7, 32, 0, 4001) for rows in (8, 20000)] == ["split"] * 2  # (the other kernels load eight columns)
     L = q.lib()
     assert [L.qmoe_hook_int4_kernel(*bad) for bad in ((0, 8, 32, 0, 1, 256), (8, 0, 32, 0, 1, 256), (8, 8, 48, 0, 1, 256), (8, 8, 32, 0, 0, 256), (8, 8, 32, 0, 1, 0))] == [0] * 5
