@@ -37,10 +37,12 @@ _MATRIX_BYTES = ctypes.sizeof(qmoe_matrix)
 
 
 class qmoe_norm(Structure):
+    device = None  # the number of the device that it points to, where that is known (device.DeviceNorm)
     _fields_ = [("kind", c_int32), ("eps", c_float), ("weight", c_void_p), ("bias", c_void_p)]
 
 
 class qmoe_int4_matrix(Structure):
+    device = None  # as above (device.DeviceInt4Matrix)
     _fields_ = [("weights", c_void_p), ("scale_f16", c_void_p), ("zero", c_void_p),
                 ("rows", c_int32), ("cols", c_int32), ("group", c_int32), ("reserved", c_int32)]
 
@@ -399,15 +401,19 @@ def _current_device() -> int:
     return device
 
 
-def _here(*tensors, descs=()) -> None:
-    """A call is enqueued on the current device: its tensors must be there, and what its descriptors point to."""
+def _here(*tensors) -> int:
+    """A call is enqueued on the current device (returned): its tensors must be there."""
     here = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the current device is {here}")
-    for d in descs:
-        if d is not None and getattr(d, "device", here) not in (here, None):
-            raise ValueError(f"what a descriptor points to is on device {d.device}, but the current device is {here}")
+    return here
+
+
+def _points_here(desc, here: int) -> None:
+    """... and so must what a descriptor points to."""
+    if desc.device != here and desc.device is not None:
+        raise ValueError(f"what a descriptor points to is on device {desc.device}, but the current device is {here}")
 
 
 def _one_device(tensors) -> None:
@@ -450,19 +456,17 @@ def _vector(t, n: int, what: str) -> int:
     return _dev_ptr(t)
 
 
-def _norm_ptr(n, d: int, what: str):
+def _norm_ptr(n, d: int, what: str, here: int):
     """n: a qmoe_norm, an object with one in .desc and its width in .d (device.DeviceNorm), or None."""
     if n is None:
         return None
     if isinstance(n, qmoe_norm):
+        _points_here(n, here)
         return byref(n)
     if n.d is not None and n.d != d:
         raise ValueError(f"{what} is a norm of {n.d} values, not {d}")
+    _points_here(n.desc, here)
     return n.ref
-
-
-def _desc(n):
-    return n if n is None or isinstance(n, qmoe_norm) else n.desc
 
 
 def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, post=None, alpha: float = 1.0, channel_scale=None,
@@ -476,9 +480,9 @@ def qmoe_residual_norm(h, y=None, h_out=None, x=None, k: int = 1, gate=None, pos
     xp, xl = (0, 0) if x is None else _bf16_matrix(x, n * copies, d, "x")
     if ot != ht:
         raise ValueError("h_out must be of h's type")
-    _here(h, y, h_out, x, gate, channel_scale, descs=(_desc(post), _desc(pre)))
-    _check(lib().qmoe_residual_norm(hp, ht, hl, yp, yt, yl, k, _vector(gate, n * k, "gate"), _norm_ptr(post, d, "post"), alpha,
-                                    _vector(channel_scale, d, "channel_scale"), _norm_ptr(pre, d, "pre"), op, ol, xp, xl, copies, n, d,
+    here = _here(h, y, h_out, x, gate, channel_scale)
+    _check(lib().qmoe_residual_norm(hp, ht, hl, yp, yt, yl, k, _vector(gate, n * k, "gate"), _norm_ptr(post, d, "post", here), alpha,
+                                    _vector(channel_scale, d, "channel_scale"), _norm_ptr(pre, d, "pre", here), op, ol, xp, xl, copies, n, d,
                                     _stream_ptr(stream)), "qmoe_residual_norm")
 
 
@@ -544,7 +548,7 @@ def qmoe_int4_matvec(W: qmoe_int4_matrix, x_bf16, y, activation: int = ACT_NONE,
     batch, rows = x_bf16.shape[0], W.rows
     xp, xl = _bf16_matrix(x_bf16, batch, W.cols, "x")
     yp, yt, yl = _matrix(y, batch, rows // 2 if activation >= ACT_SILU_GATED else rows, "y")
-    _here(x_bf16, y, descs=(W,))
+    _points_here(W, _here(x_bf16, y))
     _check(lib().qmoe_int4_matvec(byref(W), xp, xl, batch, activation, yp, yt, yl, _stream_ptr(stream)), "qmoe_int4_matvec")
 
 
