@@ -13,7 +13,7 @@ struct Int4Args {
     const uint16_t *scale;
     const uint8_t *zero;
     const Item *items;             // device list, or nullptr: tiles of `batch` tokens of the single matrix ...
-    const int *direct;             // ... or, with this one, an item for each of max_items tokens: its expert, results 0 if that is none
+    const int *direct;             // ... or, with this one, an item for each of max_items (up to 8) tokens: its expert, results 0 if that is none
     const int *n_items_dev;
     int max_items, n_experts, batch;
     const int *perm;               // slot -> token; x rows and results by token, unless ...

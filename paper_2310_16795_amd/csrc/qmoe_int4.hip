@@ -6,8 +6,9 @@ namespace qmoe {
 namespace {
 
 constexpr int kInt4MaxSplit = 8;
-// Layer calls of up to so many tokens do without the dispatch: an item a token, a shared expert's weights read again from the caches (gated, 8 tokens, with
-// the dispatch / without: 128 experts of 768 x 3072 25 / 18 us, 8 of 2080 x 6144 52 / 47, 2 of 1024 x 4096 22 / 21; 16 tokens 28 / 22, 57 / 99, 22 / 28).
+// Layer calls of up to so many tokens do without the dispatch: an item a token, of which an expert's first one takes the others along (a slot's number is four
+// bits of a word).  Gated, 8 tokens, so / with the dispatch, us, each on an expert of its own: 128 experts of 768 x 3072 19 / 25, 64 of 1024 x 4096 22 / 27, 8 of 2080 x 6144 57 / 57; all on
+// one: 15 / 21, 16 / 21, 24 / 34 (45 with an item for each token).
 constexpr int kInt4Direct = 8;
 
 // What both kernels here share.
@@ -115,17 +116,51 @@ __device__ __forceinline__ void int4_block(f32x4 (&acc)[SIDES][TILES], const u32
     }
 }
 
-// Results of 16 tokens (of the tile t) and the SIDES tiles of rows from row on; gated: the two are one's gate and product.
-template <int SIDES>
-__device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, const f32x4 (&v)[SIDES], int t, int row, int quarter, int slot0, int ntok,
+__device__ __forceinline__ bool int4_gates(const Int4Args &a) { return a.activation == QMOE_ACT_SILU_GATED || a.activation == QMOE_ACT_GELU_GATED; }
+
+struct Int4Unit {
+    int expert, slot0, ntok;
+};
+__device__ __forceinline__ Int4Unit int4_unit(const Int4Args &a, int item, int tokens)
+{
+    if (!a.items) return {0, item * tokens, min(tokens, a.batch - item * tokens)};
+    const Item it = a.items[item];
+    return {it.expert, it.slot0, min(it.ntok, tokens)};
+}
+// Direct items: the first token of an expert takes the others along (theirs are empty, ntok 0).  A token without an expert is alone, and its results are 0.
+struct Int4Direct {
+    int expert, ntok;
+    bool none;
+    uint32_t slots;  // four bits each
+};
+__device__ __forceinline__ Int4Direct int4_direct(const Int4Args &a, int item, int lane)
+{
+    const int mine = a.direct[min(lane, a.max_items - 1)], e = __builtin_amdgcn_readlane(mine, item);
+    const bool none = e < 0 || e >= a.n_experts;
+    const uint32_t same = none ? 1u << item : (uint32_t)__ballot(lane < a.max_items && mine == e);
+    Int4Direct it{none ? 0 : e, 0, none, 0};
+#pragma unroll
+    for (int j = 0; j < kInt4Direct; j++)
+        if (same >> j & 1u) it.slots |= (uint32_t)j << (4 * it.ntok++);
+    if (same & ((1u << item) - 1u)) it.ntok = 0;
+    return it;
+}
+__device__ __forceinline__ const uint16_t *int4_x_row(const Int4Args &a, int slot)
+{
+    return a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
+}
+
+// Results of 16 tokens (of the tile t) and the SIDES tiles of rows from row on; gated: the two are one's gate and product.  slot_of: where the unit's i-th token stands.
+template <int SIDES, typename F>
+__device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, const f32x4 (&v)[SIDES], int t, int row, int quarter, int ntok, F slot_of,
                                              bool none = false)
 {
 #pragma unroll
     for (int k = 0; k < 4; k++) {
         const int in_tile = 16 * t + 4 * quarter + k;
         if (in_tile >= ntok) continue;
-        const int token = a.perm ? a.perm[slot0 + in_tile] : slot0 + in_tile;
-        const size_t out_row = a.out_by_slot ? slot0 + in_tile : token;
+        const int slot = slot_of(in_tile), token = a.perm ? a.perm[slot] : slot;
+        const size_t out_row = a.out_by_slot ? slot : token;
         const float gate = none ? 0.0f : a.gate ? a.gate[token] : 1.0f;
         if (SIDES == 2 && gated) {
             if (row < a.rows) int4_store(a, out_row, gate, row, int4_gated(v[0][k], v[SIDES - 1][k], a.activation));
@@ -137,34 +172,12 @@ __device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, cons
     }
 }
 
-__device__ __forceinline__ bool int4_gates(const Int4Args &a) { return a.activation == QMOE_ACT_SILU_GATED || a.activation == QMOE_ACT_GELU_GATED; }
-
-struct Int4Unit {
-    int expert, slot0, ntok;
-    bool none;  // a token without an expert: its results are 0
-};
-__device__ __forceinline__ Int4Unit int4_unit(const Int4Args &a, int item, int tokens)
-{
-    if (a.direct) {
-        const int e = a.direct[item];
-        const bool none = e < 0 || e >= a.n_experts;
-        return {none ? 0 : e, item, 1, none};
-    }
-    if (!a.items) return {0, item * tokens, min(tokens, a.batch - item * tokens), false};
-    const Item it = a.items[item];
-    return {it.expert, it.slot0, min(it.ntok, tokens), false};
-}
-__device__ __forceinline__ const uint16_t *int4_x_row(const Int4Args &a, int slot)
-{
-    return a.x + (size_t)(a.perm && !a.x_by_slot ? a.perm[slot] : slot) * a.ld_x;
-}
-
 // Little work: a workgroup's wavefronts share 16 rows (gated: of each projection) along the columns, each with its own piece of LDS for the
 // activations of its block, so that none waits for another before all join their sums, in a fixed order.
 // Bound by latency: 4096 x 1024, one token (2.2 MB) 5.2 us (k_route of one token, a launch with next to no work, is 2.2 in the same trace); 2080 x 6144 with zero points, 37 tokens (7.1 MB) 13 us,
 // six blocks one after the other in each of 3120 wavefronts, 2080 x 6144 with one token 7.4 us (0.9 TB/s).  Two tiles of rows a wavefront (half the
 // activations' reads) lost wherever this kernel is taken (2080 x 6144, 16 tokens 9.9 -> 12, 64 tokens 17.6 -> 19).
-template <int SIDES, int PER_BLOCK>
+template <int SIDES, int PER_BLOCK, bool DIRECT>
 __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Args a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -176,14 +189,25 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
     f32x4 *joined = reinterpret_cast<f32x4 *>(smem);
     const bool gated = int4_gates(a);
     const int row_tiles = (a.rows + 15) / 16;
-    const int n_items = a.direct ? a.max_items : a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
+    const int n_items = DIRECT ? a.max_items : a.items ? min(*a.n_items_dev, a.max_items) : (a.batch + TOKENS - 1) / TOKENS;
     const long long total = (long long)n_items * row_tiles;
     const int b0 = (int)((long long)a.blocks * part / a.split), b_end = (int)((long long)a.blocks * (part + 1) / a.split);
     for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
         const int item = (int)(unit / row_tiles), tile = (int)(unit - (long long)item * row_tiles);
-        const Int4Unit it = int4_unit(a, item, TOKENS);
-        const int b1 = it.none ? b0 : b_end;
-        const Int4Matrix m = int4_matrix(a, it.expert);
+        int expert, slot0 = 0, ntok;
+        uint32_t slots = 0;
+        bool none = false;
+        if constexpr (DIRECT) {
+            const Int4Direct it = int4_direct(a, item, lane);
+            if (it.ntok == 0) continue;  // (the same for the workgroup)
+            expert = it.expert, ntok = it.ntok, slots = it.slots, none = it.none;
+        } else {
+            const Int4Unit it = int4_unit(a, item, TOKENS);
+            expert = it.expert, slot0 = it.slot0, ntok = it.ntok;
+        }
+        const int b1 = none ? b0 : b_end;
+        auto slot_of = [&](int i) { return DIRECT ? (int)(slots >> (4 * i) & 15u) : slot0 + i; };
+        const Int4Matrix m = int4_matrix(a, expert);
         Int4Rows<SIDES, 1, PER_BLOCK> rows;
         int base[SIDES], behind[SIDES];
 #pragma unroll
@@ -192,12 +216,12 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
         const uint16_t *x_row[4];
 #pragma unroll
         for (int j = 0; j < 4; j++)
-            if (4 * j < it.ntok) x_row[j] = int4_x_row(a, it.slot0 + min(4 * j + quarter, it.ntok - 1));
+            if (4 * j < ntok) x_row[j] = int4_x_row(a, slot_of(min(4 * j + quarter, ntok - 1)));
         u32x4 x_next[4], w_next[1][SIDES];
         auto load_x = [&](int b) {
 #pragma unroll
             for (int j = 0; j < 4; j++)
-                if (4 * j < it.ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * n16, a.cols, kInt4BlockCols * (b + 1) <= a.cols);
+                if (4 * j < ntok) x_next[j] = int4_x(x_row[j], kInt4BlockCols * b + 8 * n16, a.cols, kInt4BlockCols * (b + 1) <= a.cols);
         };
         f32x4 acc[SIDES][1];
 #pragma unroll
@@ -213,7 +237,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
             __builtin_amdgcn_wave_barrier();  // the block before has been read
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                if (4 * j >= it.ntok) continue;
+                if (4 * j >= ntok) continue;
                 *reinterpret_cast<u32x4 *>(&s_x[(4 * j + quarter) * LD + 8 * n16]) = x_next[j];
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -250,7 +274,7 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
                 v[g] = joined[g * 64 + lane];
                 for (int p = 1; p < a.split; p++) v[g] += joined[(p * SIDES + g) * 64 + lane];
             }
-            int4_results<SIDES>(a, gated, v, 0, 16 * tile + n16, quarter, it.slot0, it.ntok, it.none);
+            int4_results<SIDES>(a, gated, v, 0, 16 * tile + n16, quarter, ntok, slot_of, none);
         }
         __syncthreads();  // before the next unit's activations overwrite these
     }
@@ -395,7 +419,7 @@ __global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int
         for (int t = 0; t < TILES; t++) {
             if (16 * t >= it.ntok) break;
             const f32x4 v[2] = {acc[0][t], acc[1][t]};
-            int4_results<2>(a, gated, v, t, first + n16, quarter, it.slot0, it.ntok);
+            int4_results<2>(a, gated, v, t, first + n16, quarter, it.ntok, [&](int i) { return it.slot0 + i; });
         }
     }
 }
@@ -418,9 +442,10 @@ qmoe_status launch_split_variant(const Int4Args &a, int grid, hipStream_t s)
 {
     const size_t x = a.split * (16 * (kInt4BlockCols + 8) * 2);
     const size_t smem = std::max(x, (size_t)a.split * SIDES * 64 * sizeof(f32x4));
-    const qmoe_status st = allow_lds(k_int4_split<SIDES, PER_BLOCK>, smem);
+    const auto kernel = a.direct ? k_int4_split<SIDES, PER_BLOCK, true> : k_int4_split<SIDES, PER_BLOCK, false>;
+    const qmoe_status st = allow_lds(kernel, smem);
     if (st != QMOE_OK) return st;
-    hipLaunchKernelGGL((k_int4_split<SIDES, PER_BLOCK>), dim3(grid), dim3(64 * a.split), smem, s, a);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * a.split), smem, s, a);
     QMOE_HIP_TRY(hipGetLastError());
     return QMOE_OK;
 }

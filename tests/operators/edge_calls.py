@@ -76,12 +76,17 @@ def layer_groups(rng, i):
     return calls.layer(_Groups(rng, [256, 384, 512, 1152][i // 4 % 4]), i, sizes)
 
 
+def layer_few(rng, i):
+    """Up to eight tokens, many on one expert."""
+    return calls.layer(rng, i, (int(rng.choice([1, 2, 3])), i % 8 + 1, 8 * int(rng.integers(1, 40)), 8 * int(rng.integers(1, 40))))
+
+
 if __name__ == "__main__":
     kind, count = sys.argv[1], int(sys.argv[2])
     rng, ok = np.random.default_rng(7), True
     for i in range(count):
         before = L.lanes_reports()
-        right = {"outlier": outlier, "wide": wide, "layer_groups": layer_groups}[kind](rng, i)
+        right = {"outlier": outlier, "wide": wide, "layer_groups": layer_groups, "layer_few": layer_few}[kind](rng, i)
         out = L.lanes_reports() - before
         ok &= bool(right) and out == 0
         if not right or out:

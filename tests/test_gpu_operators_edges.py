@@ -163,3 +163,19 @@ def test_int4_layer_kernels(gpu, kernels, E, d_model, d_ff, T, group, zeros, act
     _untouched(held, T, d_model)
     layer.forward(x, *args)
     assert torch.equal(y, first)
+
+
+@pytest.mark.parametrize("idx", [[0] * 8, [2, 2, 1, 2, -1, 1, 2, 5], [1, 0, 1, 0, 1, 0, 1], [3, -1, 3, 99, 3], [4, 4], [-1] * 6, [0, 1, 2, 3, 4, 4, 3, 2]])
+@pytest.mark.parametrize("act,zeros,group", [("relu", False, 128), ("silu", True, 64), ("gelu", True, 256)])
+def test_int4_layer_of_few_tokens_that_share_experts(gpu, idx, act, zeros, group):  # noqa: F811
+    """Up to eight tokens go without the dispatch; those of one expert are multiplied together, each where it stands."""
+    rng = np.random.default_rng(len(idx))
+    E, d_model, d_ff, T = 5, 392, 520, len(idx)
+    ex, layer = _layer(gpu, rng, E, d_model, d_ff, group, zeros, act)
+    idx = np.array(idx, dtype=np.int32)
+    gate = rng.random(T).astype(np.float32)
+    x, x64 = _up(rng.standard_normal((T, d_model)), gpu, "bf16")
+    (y, held), ws = _out(T, d_model, gpu, "f32"), layer.workspace(T)
+    layer.forward(x, torch.from_numpy(idx).to(gpu), y, ws, torch.from_numpy(gate).to(gpu))
+    _check_layer(ex, x64, idx, gate, group, act, "f32", y.cpu(), ws, d_model, d_ff)
+    _untouched(held, T, d_model)

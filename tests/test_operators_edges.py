@@ -14,7 +14,7 @@ from test_operators_lanes import library  # noqa: F401
 HERE = os.path.dirname(os.path.abspath(__file__))
 
 
-@pytest.mark.parametrize("kind,count,units", [("outlier", 32, 1), ("outlier", 16, 64), ("wide", 16, 1), ("wide", 8, 6), ("layer_groups", 16, 1), ("layer_groups", 16, 8)])
+@pytest.mark.parametrize("kind,count,units", [("outlier", 32, 1), ("outlier", 16, 64), ("wide", 16, 1), ("wide", 8, 6), ("layer_groups", 16, 1), ("layer_groups", 16, 8), ("layer_few", 24, 2), ("layer_few", 24, 256)])
 def test_edge_calls(library, kind, count, units):  # noqa: F811
     cmd = [sys.executable, os.path.join(HERE, "operators", "edge_calls.py"), kind, str(count)]
     r = subprocess.run(cmd, env={**os.environ, "QMOE_LIBRARY": library, "LANES_COMPUTE_UNITS": str(units)}, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=600)
