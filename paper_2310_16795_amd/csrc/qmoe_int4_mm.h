@@ -34,6 +34,7 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
     const int n_items = (a.batch + TOKENS - 1) / TOKENS;
     const long long total = (long long)n_items * row_blocks;
     const size_t row_bytes = (size_t)64 * a.blocks;
+    const Int4Matrix m{a.weights, (gp_u16)a.scale, (gp_bytes)a.zero};
     for (long long unit = blockIdx.x; unit < total; unit += gridDim.x) {
         // Workgroups go to the eight XCDs in turn: an XCD's units follow each other and go by eight tiles of tokens, so that what it holds at a
         // time shares rows and activations in its L2.
@@ -42,7 +43,6 @@ __global__ __launch_bounds__(256, 2) void k_int4_mm(const Int4Args a)
         const int group = (int)(at / (8LL * row_blocks)), in = (int)(at - group * 8LL * row_blocks);
         const int wide = group < tiles8 ? 8 : n_items - 8 * tiles8;
         const int rb = in / wide, token0 = (8 * group + in % wide) * TOKENS, ntok = min(TOKENS, a.batch - token0);
-        const Int4Matrix m = int4_matrix(a, 0);
         const int first = 16 * OUT_TILES * (4 * rb + wave);  // row of this wavefront
         // the matrix's row that a tile's row is
         auto row_of = [&](int r, int in_tile) {

@@ -1,5 +1,5 @@
 // Shared by the operators around the ternary layer: residual stream and norm (qmoe_norm.hip), the router's choice
-// (qmoe_route.hip), four-bit weights (qmoe_int4.hip, qmoe_int4_mm.hip).  Each unit holds its kernels and its C entry points.
+// (qmoe_route.hip), four-bit weights (qmoe_int4.hip, qmoe_int4_mm_*.hip).  Each unit holds its kernels and its C entry points.
 // Not part of the C ABI.
 #pragma once
 
@@ -9,8 +9,7 @@ namespace qmoe {
 
 // ---- from qmoe_api.hip
 qmoe_status gpu_info(DeviceInfo *out);
-// Tokens grouped by expert in a layer workspace: the experts with few tokens in tiles of one size (few), the others in tiles of
-// up to kMmTokens (many), the lists' lengths on the device; slot -> token, and the place of the hidden vectors by slot.
+// Tokens grouped by expert in a layer workspace: one list of tiles, its length on the device; slot -> token, and the place of the hidden vectors by slot.
 struct GroupedTokens {
     const Item *items;
     const int *n_items, *perm;

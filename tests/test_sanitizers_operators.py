@@ -2,11 +2,12 @@
 form and the quantiser of four-bit weights, and the entry points' argument checks and choices of kernels."""
 import os
 import subprocess
+import sys
 
 import pytest
 
-from test_sanitizers import CSRC, ROOT, _run_child
-
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2310_16795_amd", "csrc")
 UNITS = ["qmoe_int4_host.cpp", "qmoe_host.cpp", "qmoe_api.hip", "qmoe_norm.hip", "qmoe_route.hip", "qmoe_int4.hip"]
 HOST_ONLY = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined"]
 
@@ -32,4 +33,9 @@ def test_operators_host_side_under_asan_and_ubsan(tmp_path):
     subprocess.check_call(["hipcc", "-shared", "-fPIC", "--offload-arch=gfx950", *HOST_ONLY[:4], "-shared-libsan", "-o", lib, *objects, *others])
     names = subprocess.check_output(["nm", objects[0]], text=True)
     assert "__asan_report" in names and "__ubsan_handle" in names  # instrumented
-    _run_child(["tests/test_operators_host.py"], {"QMOE_LIBRARY": lib}, runtimes[0])
+    env = {**os.environ, "QMOE_LIBRARY": lib, "LD_PRELOAD": " ".join(x for x in (os.environ.get("LD_PRELOAD"), runtimes[0]) if x),
+           "ASAN_OPTIONS": "detect_leaks=0:verify_asan_link_order=0:abort_on_error=0:exitcode=23",
+           "UBSAN_OPTIONS": "halt_on_error=1:print_stacktrace=1:exitcode=23"}
+    r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-m", "not gpu", "-p", "no:cacheprovider", "tests/test_operators_host.py"], cwd=ROOT, env=env,
+                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0 and "passed" in r.stdout, r.stdout[-4000:]
