@@ -174,9 +174,8 @@ __device__ __forceinline__ void int4_results(const Int4Args &a, bool gated, cons
 
 // Little work: a workgroup's wavefronts share 16 rows (gated: of each projection) along the columns, each with its own piece of LDS for the
 // activations of its block, so that none waits for another before all join their sums, in a fixed order.
-// Bound by latency: 4096 x 1024, one token (2.2 MB) 5.2 us (k_route of one token, a launch with next to no work, is 2.2 in the same trace); 2080 x 6144 with zero points, 37 tokens (7.1 MB) 13 us,
-// six blocks one after the other in each of 3120 wavefronts, 2080 x 6144 with one token 7.4 us (0.9 TB/s).  Two tiles of rows a wavefront (half the
-// activations' reads) lost wherever this kernel is taken (2080 x 6144, 16 tokens 9.9 -> 12, 64 tokens 17.6 -> 19).
+// Bound by latency: 4096 x 1024, one token (2.2 MB) 5.2 us (k_route of one token, a launch with next to no work, is 2.2 in the same trace); 2080 x 6144 with zero points, 37 tokens (7.1 MB) 12 us,
+// six blocks one after the other in each of 3120 wavefronts, 2080 x 6144 with one token 6.5 us (1 TB/s).
 template <int SIDES, int PER_BLOCK, bool DIRECT>
 __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Args a)
 {
@@ -286,9 +285,10 @@ __global__ __launch_bounds__(64 * kInt4MaxSplit) void k_int4_split(const Int4Arg
 // another.
 // The scales and zero points of AT_ONCE groups go through LDS, too, a wavefront's own: a row's few bytes a step, asked for step by step, would
 // be the same lines of memory again and again, gone from the caches in between.
-// Few tokens an expert: memory, 64 tokens on 57 of 256 gated experts of 2080 x 6144 (1.17 GB) 260 us for both products, 4.5 TB/s where a large copy has 4.9.
-// More: the vector instructions of decoding and scaling and each unit's start, 128 experts of 768 x 3072, 4001 tokens (38 GFLOP, 310 MB) 163 us:
-// vector instructions take 43 us of the first product and 32 of the second (70-76 each), the matrix cores 13.  32 tokens a tile at three wavefronts a SIMD 167, at two 174.
+// Few tokens an expert: memory and decoding, 64 tokens on 57 of 256 gated experts of 2080 x 6144 (1.17 GB) 284 us for both products, 4.1 TB/s where a large copy
+// has 4.9; vector instructions, three quarters of them int4_weights, are issued in 75 % of the first product's cycles.
+// More: 128 experts of 768 x 3072, 4001 tokens (38 GFLOP, 310 MB) 168 us: vector instructions in 53 % of the cycles of either product, the matrix cores in 15, and the
+// starts of 6072 and 1518 units of three and twelve steps, which one of three wavefronts a SIMD waits for.
 template <int TILES, int PER_BLOCK>
 __global__ __launch_bounds__(256, TILES == 1 ? 4 : 3) void k_int4_tile(const Int4Args a)
 {
@@ -518,9 +518,9 @@ qmoe_status launch_way(Int4Args a, const Int4Way &way, long long items, int cus,
     return way.tiles == 1 ? launch_tile<1>(a, grid, s) : launch_tile<2>(a, grid, s);
 }
 
-// One matrix: the kernel for many tokens where it fills the GPU one and a half times (12288 x 2080, 256 tokens 39 us, the other way 32; 512 53 /
-// 56; 1024 84 / 103).  In layer calls, where tiles are partly empty, it lost (16 experts of 1024 x 4096, 4001 tokens 213, the other way 182;
-// 64 of 1024 x 2048, 1000 tokens 122 / 68).
+// One matrix: the kernel for many tokens where it fills the GPU one and a half times (12288 x 2080, 256 tokens 37 us, the other way 35; 512 52 /
+// 61; 1024 77 / 110).  In layer calls, where tiles are partly empty, it lost (16 experts of 1024 x 4096, 4001 tokens 213, the other way 182;
+// 64 of 1024 x 2048, 1000 tokens 122 / 68, both with the earlier decoding).
 long long mm_units(const Int4Args &a)
 {
     const int rows = int4_is_gated(a.activation) ? 128 : 256;

@@ -13,10 +13,10 @@ namespace {
 // them, so that decoding one tile runs beside multiplying the one before and few registers hold operands.  Two wavefronts a SIMD: the
 // sums (64 registers) are scaled into the result (64) in fp32, which accumulation registers could not take part in.
 // Scales and zero points of kMmAtOnce groups lie in LDS, a wavefront's own.
-// 12288 x 2080 (gated, groups of 128), 4001 tokens: 263 us, 780 TFLOP/s; the matrix cores are busy for 86 us of it, vector instructions (decoding 34 %,
-// scaling 15, group sums and epilogue the rest) for 137, and the two overlap in part.  The library's bf16 product of that shape is 196 us, without the activation.
-// Without gain: operands straight from memory, other orders of tokens and rows, wave priorities, matrix and vector
-// instructions interleaved by hand (282 then).
+// 12288 x 2080 (gated, groups of 128), 4001 tokens: 271 to 281 us back to back, 730 to 760 TFLOP/s; of a launch's cycles vector instructions are issued in 63 % (decoding is 53 %
+// of them, scaling 13), the matrix cores are busy in 31 and LDS in about 40, its bank conflicts among them, at two wavefronts a SIMD and with a barrier a step: three pipes that overlap in part.
+// The library's bf16 product of that shape is 196 us, without the activation.  With zero points 300, groups of 64 332, groups of 32 412: the zero points' constants spill 50 to 120
+// bytes a lane.
 constexpr int kMmRows = 4, kMmTiles = 4, kMmAtOnce = 32;
 
 template <bool GATED, bool ZEROS, int PER_BLOCK>

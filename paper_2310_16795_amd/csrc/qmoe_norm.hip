@@ -91,7 +91,7 @@ __global__ __launch_bounds__(ALONE ? 256 : 1024) void k_residual_norm(const Norm
     const long long row = alone ? (long long)blockIdx.x * (blockDim.x >> 6) + wave : blockIdx.x;
     if (row >= a.n_tokens) return;  // (a workgroup of one row leaves as one)
     const int me = alone ? lane : (int)threadIdx.x, step = 64 * a.waves * 8;
-    // the longest rows fill the registers: their quarters are not to be loaded ahead of each other (512 rows of 32768 54 us, spilled 97)
+    // the longest rows fill the registers: their quarters are not to be loaded ahead of each other (512 rows of 32768, all fp32, 56 us, 4.2 TB/s; spilled 97)
     auto apart = [] {
         if constexpr (PER == 4) __builtin_amdgcn_sched_barrier(0);
     };

@@ -136,8 +136,8 @@ __device__ __forceinline__ void four_logits(float (&v)[4], const void *base, siz
 // A token's keys lie in the registers of LANES lanes, four neighbouring experts in a lane's four registers, then those 4 * LANES further: one
 // pass over memory.  Each of the k rounds takes the largest key (a reduction over the lanes), of equal ones that of the lowest
 // index (a second one), and the lane that held it looks for its next best.
-// With many experts memory bounds it: 4096 tokens of 2048 fp32 logits (34 MB) 9.4 us, 3.6 TB/s; with few instruction issue
-// does: 16384 tokens of 256 bf16 logits, best eight, 10.7 us for 9.4 MB, 1280 vector instructions a wavefront of four tokens (8.5 us), two thirds of them
+// With many experts memory bounds it: 4096 tokens of 2048 fp32 logits (34 MB) 9.8 us, 3.4 TB/s; with few instruction issue
+// does: 16384 tokens of 256 bf16 logits, best eight, 10.6 us for 9.4 MB, 1280 vector instructions a wavefront of four tokens, two thirds of them
 // looking for the next best of 16 keys.  Keeping each lane's second best, too, was 17: with eight of 16 lanes' keys to take, some lane of four tokens needs
 // its third in nearly every round.  16 lanes a token up to 256 experts keep the reductions inside
 // a row of the wavefront (four DPP steps) and four tokens in one instruction.
@@ -207,8 +207,8 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a)
 }
 
 // More experts than a wavefront's registers hold: a workgroup a token, its keys in the registers of 512 lanes.  The rounds are k_route's, joined over the
-// wavefronts through LDS, one barrier each (two places in turn).  4096 tokens of 4096 experts, best eight: 61 us; 64 of 16384: 12; reading the
-// logits again for every round took 119 and 119.
+// wavefronts through LDS, one barrier each (two places in turn).  4096 tokens of 4096 experts, best eight: 60 us; 64 of 16384: 12; reading the
+// logits again for every round took 119 and 119.  The rounds bound it, as above: the reading takes 14 and less than 1.
 constexpr int kWideLanes = 512;
 
 template <int TYPE, int PER>
